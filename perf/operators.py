@@ -171,7 +171,7 @@ def _quantise(x):
     """Rows of x (last axis) to codes, step size and least value, each step one binary32 operation."""
     x = x.float()
     low, high = x.amin(-1, keepdim=True), x.amax(-1, keepdim=True)
-    step = ((high - low) / 15).clamp(2.0 ** -24, 65504.0).half()
+    step = ((high - low) * (1.0 / 15.0)).clamp(2.0 ** -24, 65504.0).half()
     low = low.clamp(-65504.0, 65504.0).half()
     codes = ((x - low.float()) / step.float()).round().clamp(0, 15).to(torch.uint8)
     return codes, step.squeeze(-1), low.squeeze(-1)
@@ -423,10 +423,10 @@ def run(s):
                                           case["interleaved"])
             return [t for t in got if t is not None]
         if path == "append":
-            B.kv4_append(s["pages"], s["table"], s["starts"], s["lengths"], s["k"], s["v"], max_new=s["max_new"])
-            return B.kv4_read(s["pages"], s["table"], s["rows"], s["total"], case["dim"], max_len=s["max_len"])
+            B.cache_append(s["pages"], s["table"], s["starts"], s["lengths"], s["k"], s["v"], max_new=s["max_new"])
+            return B.cache_read(s["pages"], s["table"], s["rows"], s["total"], case["dim"], max_len=s["max_len"])
         if path == "attend":
-            return B.kv4_attention(s["q"], s["pages"], s["table"], s["starts"], s["lengths"], window=case["window"], sinks=case["sinks"],
+            return B.cache_attention(s["q"], s["pages"], s["table"], s["starts"], s["lengths"], window=case["window"], sinks=case["sinks"],
                                    max_new=s["max_new"], max_len=s["max_len"])
         return B.sample(s["logits"], s["noise"], s["temperature"], s["top_k"], s["top_p"], s["min_p"])
     return {"rope": _rope_plain, "rope_bwd": _rope_bwd_plain, "append": _append_plain, "attend": _attend_plain,

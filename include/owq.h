@@ -47,7 +47,8 @@ typedef enum {
   OWQ_ERR_HIP = 10,       /* a HIP call failed; see owq_layer_info_t.last_hip_error */
   OWQ_ERR_UNSUPPORTED = 11, /* the layer needs more on-chip memory than one workgroup may use */
   OWQ_ERR_LAYOUT = 12,     /* layout is none of OWQ_LAYOUT_GEMV, OWQ_LAYOUT_TILE, OWQ_LAYOUT_COMPACT */
-  OWQ_ERR_SCRATCH = 13     /* owq_linear_static: the layer needs more than OWQ_STATIC_SCRATCH_BYTES of scratch memory */
+  OWQ_ERR_SCRATCH = 13,    /* owq_linear_static: the layer needs more than OWQ_STATIC_SCRATCH_BYTES of scratch memory */
+  OWQ_ERR_TYPE = 14        /* a type is none of the OWQ_TYPE_* that the call takes */
 } owq_status_t;
 
 #define OWQ_MAX_BATCH 65535
@@ -369,6 +370,170 @@ owq_status_t owq_search_config(const owq_search_desc_t *desc, const uint16_t *w,
 owq_status_t owq_backward_workspace_bytes(owq_handle_t h, int32_t batch, size_t *bytes);
 owq_status_t owq_linear_backward(owq_handle_t h, const void *dy, const void *x, void *dx, float *dww,
                                  int32_t batch, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The operators between two low-bit layers of a decoder: norm of every query and key head with
+ * the position rotation, a cache of keys and values in 4 bits, attention over it, and the choice
+ * of a token from logits.  None of them needs a handle; every pointer but the descriptions is
+ * DEVICE memory owned by the caller; work is enqueued on `stream`, nothing is allocated, copied
+ * or waited for, and every result is reproducible bit for bit.  Strides count elements; the
+ * last axis of every tensor is contiguous; rows of fp16 or bf16 heads begin on 16-byte
+ * boundaries (base pointers and strides in multiples of 8 elements, else OWQ_ERR_BUFFER).
+ */
+#define OWQ_TYPE_F16 0
+#define OWQ_TYPE_BF16 1
+#define OWQ_TYPE_F32 2
+
+/*
+ * Head norm and rotation.  With x a head of q or k of one token, w the weight (wq or wk), p the
+ * token's position and R = rotary_dim:
+ *     n = x / sqrt(mean(x^2) + eps) * w           (n = x where that weight is NULL)
+ *     y[a_j] = n[a_j] cos[p][j] - n[b_j] sin[p][j],  y[b_j] = n[b_j] cos[p][j] + n[a_j] sin[p][j]
+ *     (a_j, b_j) = (j, j + R / 2), or (2 j, 2 j + 1) if interleaved, j < R / 2;  y = n elsewhere
+ * in binary32, rounded once.  A position outside [0, n_positions) makes that token's rotated
+ * elements NaN (nothing is read out of bounds).
+ *   q [n_tokens][q_heads][head_dim], k [n_tokens][kv_heads][head_dim] of `type`, with strides
+ *   wq, wk [head_dim] of `type` or NULL;  cos, sin fp32 [n_positions][rotary_dim / 2]
+ *   positions int32 [n_tokens];  q_out, k_out packed, written in full; each may be its input
+ * where that is packed too.
+ * head_dim a multiple of 8 up to 256 and rotary_dim a multiple of 16 in [16, head_dim] (else
+ * OWQ_ERR_UNSUPPORTED), type OWQ_TYPE_F16 or OWQ_TYPE_BF16 (else OWQ_ERR_TYPE), kv_heads may be
+ * 0 (k and k_out are not used then).  n_tokens == 0 is a no-op.
+ *
+ * The backward takes the gradients of q_out and k_out and gives those of q, k (packed) and, in
+ * fp32 and summed over all tokens and heads, of the weights (NULL = not wanted; a weight that is
+ * NULL has none).  With g the gradient turned back, r = 1 / sqrt(mean(x^2) + eps), h = g w:
+ *     dw = sum g x r,   dx = r (h - x r^2 mean(h x))          (dx = g without a weight)
+ * workspace: owq_qk_norm_rope_backward_workspace_bytes bytes, 16-byte aligned, contents
+ * undefined before and after (may be NULL if the answer is 0: no weight, or no gradient of one wanted).
+ */
+typedef struct {
+  int32_t n_tokens, q_heads, kv_heads, head_dim, rotary_dim;
+  int32_t interleaved, type, n_positions;
+  float eps;
+  int32_t reserved;                            /* 0 */
+  int64_t q_token, q_head, k_token, k_head;    /* strides of q and k */
+  int64_t dq_token, dq_head, dk_token, dk_head; /* backward: strides of the incoming gradients */
+} owq_rope_desc_t;
+
+owq_status_t owq_qk_norm_rope(const owq_rope_desc_t *desc, const void *q, const void *k, const void *wq, const void *wk,
+                              const float *cos, const float *sin, const int32_t *positions, void *q_out, void *k_out,
+                              void *stream);
+owq_status_t owq_qk_norm_rope_backward_workspace_bytes(const owq_rope_desc_t *desc, size_t *bytes);
+owq_status_t owq_qk_norm_rope_backward(const owq_rope_desc_t *desc, const void *dq_out, const void *dk_out, const void *q,
+                                       const void *k, const void *wq, const void *wk, const float *cos, const float *sin,
+                                       const int32_t *positions, void *dq, void *dk, float *dwq, float *dwk,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Keys and values of a decoder layer in 4 bits, in pages.  Per token and key/value head the
+ * head_dim values x are stored as codes c with an fp16 step size s and least value lo:
+ *     lo = fp16(min x),  s = fp16((max x - min x) * fp32(1/15)), at least 2^-24,
+ *     c = clamp(rint((x - lo) / s), 0, 15),   the value it stands for: s c + lo
+ * each step one binary32 operation, lo and s clamped to the finite fp16 values.  A head with an
+ * infinity or a NaN in it gets s = lo = NaN and codes 0: it makes NaN of whatever sees it.
+ *
+ * pages: [n_pages][kv_heads][page_size / 32] tiles of 32 tokens, a tile of 32 P + 256 bytes, P =
+ * head_dim rounded up to 32 (columns past head_dim hold code 0): the keys' codes, the values'
+ * codes (16 P bytes each), then (s, lo) of 32 keys and of 32 values, fp16 pairs.  Codes are
+ * 32-bit words in the order of matrix-core operands, [P / 32][4][16][2]:
+ *     keys    word (S, q, r, h): token 16 h + r, columns 32 S + 8 q + e
+ *     values  word (S, q, r, j): tokens 16 (e / 4) + 4 q + e % 4, column 32 S + 16 j + r
+ * with element e = 0..7 at bits 4 (e / 2 + 4 (e % 2)) and up.  16-byte aligned.
+ * page_table int32 [n_seqs][table_stride]: page t / page_size of sequence b holds its token t;
+ * entries outside [0, n_pages) stand for no page: tokens there are neither written nor seen.
+ * Pages may be shared by sequences that only read them.
+ * Requires head_dim a multiple of 8 up to 128, page_size a power of two from 32 to 65536 (else
+ * OWQ_ERR_UNSUPPORTED), n_seqs up to 65535; offsets are 64-bit throughout.
+ *
+ * Sequences are ragged: sequence b owns rows starts[b] .. starts[b + 1] - 1 of the row tensors
+ * (starts int32 [n_seqs + 1], ascending; rows outside [0, n_rows) are never touched), and
+ * lengths[b] is its number of tokens in the cache, the new ones included: row starts[b] + i has
+ * position lengths[b] - (starts[b + 1] - starts[b]) + i.
+ */
+typedef struct {
+  int32_t n_pages, page_size, kv_heads, head_dim;
+  int32_t n_seqs, table_stride;
+} owq_cache_desc_t;
+
+/* Bytes of one page (all its heads). */
+owq_status_t owq_cache_page_bytes(const owq_cache_desc_t *desc, size_t *bytes);
+
+/*
+ * Write the new rows of k and v, [n_rows][kv_heads][head_dim] of `type` with strides, into the
+ * cache; rows with a negative position are left out.  max_new: no sequence has more new rows
+ * (rows past it are not written).  Other tokens of a tile keep their contents.  Pages that
+ * receive tokens of two sequences in one call race; calls in flight at once on one page race.
+ */
+owq_status_t owq_cache_append(const owq_cache_desc_t *desc, void *pages, const int32_t *page_table, const int32_t *starts,
+                              const int32_t *lengths, const void *k, const void *v, int32_t type, int32_t n_rows,
+                              int32_t max_new, int64_t k_row, int64_t k_head, int64_t v_row, int64_t v_head, void *stream);
+
+/*
+ * The reverse: tokens 0 .. starts[b + 1] - starts[b] - 1 of every sequence, as values s c + lo
+ * (one binary32 operation) rounded to `type`, into k_out and v_out [n_rows][kv_heads][head_dim],
+ * packed.  max_len: no sequence has more (rows past it are not written).  Tokens on no page read 0.
+ */
+owq_status_t owq_cache_read(const owq_cache_desc_t *desc, const void *pages, const int32_t *page_table,
+                            const int32_t *starts, void *k_out, void *v_out, int32_t type, int32_t n_rows, int32_t max_len,
+                            void *stream);
+
+/*
+ * Attention of the new rows over the cache.  q [n_rows][q_heads][head_dim] of `type` with
+ * strides, query head h on key/value head h / (q_heads / kv_heads) (q_heads a multiple of
+ * kv_heads, else OWQ_ERR_SHAPE).  A row at position p sees the tokens t <= p with window == 0 or
+ * t > p - window or t < sinks:
+ *     y_t = scale q . (s_t c_t + lo_t),   out = sum_t softmax(y)_t (s'_t c'_t + lo'_t)
+ * out [n_rows][q_heads][head_dim] of `type`, packed; lse fp32 [n_rows][q_heads], ln sum exp y,
+ * or NULL.  A row that sees nothing gets 0 and -infinity.  An infinity or NaN in a query or in
+ * a cached head that it sees makes its row NaN; what is masked has no effect, whatever its bits.
+ * max_new, max_len: no sequence has more new rows or tokens (rows past max_new are not written,
+ * tokens past max_len are not seen); smaller bounds mean fewer empty workgroups.
+ * Scores and sums are fp32; the softmax weights times the values' step sizes are rounded to fp16
+ * once (relative 2^-11 per token) for the matrix cores; out is rounded once.
+ * workspace: owq_cache_attention_workspace_bytes bytes for the same description and the same
+ * n_rows, max_new, max_len, q_heads, window and sinks, 256-byte aligned (may be NULL if the
+ * answer is 0), contents undefined before and after.
+ */
+typedef struct {
+  int32_t q_heads, type, n_rows, max_new, max_len;
+  int32_t window, sinks;      /* 0 = none */
+  float scale;
+  int64_t q_row, q_head;      /* strides of q */
+} owq_attention_desc_t;
+
+owq_status_t owq_cache_attention_workspace_bytes(const owq_cache_desc_t *desc, const owq_attention_desc_t *att, size_t *bytes);
+owq_status_t owq_cache_attention(const owq_cache_desc_t *desc, const owq_attention_desc_t *att, const void *q,
+                                 const void *pages, const int32_t *page_table, const int32_t *starts,
+                                 const int32_t *lengths, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * One token per row of logits [n_rows][vocab] of `type` (any OWQ_TYPE_*; row stride logits_row),
+ * from given random numbers: noise fp32 [n_rows][vocab] (row stride noise_row), independent
+ * exponential variates e.  With z = logits / temperature[row]:
+ *   1. the top_k[row] largest logits stay (top_k < 1: all), of equal ones the lower index;
+ *   2. of these, in descending order, those with less than top_p[row] of their probability
+ *      (softmax of z over what stayed) before them: never none, all if top_p >= 1;
+ *   3. of these, those with z >= max z + ln min_p[row] (min_p <= 0: all).
+ * token[row] = the one with the largest z - ln e (the lower index of equal ones): each stays
+ * with its softmax probability over what is left.  temperature[row] == 0: the largest logit.
+ * temperature, top_k, top_p, min_p: [n_rows], or NULL for 1, all, 1, 0; noise may be NULL only
+ * if temperature is given, and is read at tokens that stay only.
+ * logprob[row] (may be NULL) = z[token] - ln sum exp z over the whole vocabulary (with
+ * temperature 1 where it is 0).  Logits of -infinity are never chosen.  A row whose largest
+ * logit is not finite, or that has a NaN in it, or whose temperature is negative or NaN, has no
+ * token: -1 and NaN; so has a row whose temperature is not 0 without noise.
+ * Probabilities are summed in 40-bit fixed point, so no order of summation shows.
+ * n_rows == 0 is a no-op; vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
+ * workspace: owq_sample_workspace_bytes bytes, 16-byte aligned (may be NULL if the answer is 0),
+ * contents undefined before and after.
+ */
+owq_status_t owq_sample_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t type, size_t *bytes);
+owq_status_t owq_sample(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row,
+                        const float *noise, int64_t noise_row, const float *temperature, const int32_t *top_k,
+                        const float *top_p, const float *min_p, int32_t *token, float *logprob, void *workspace,
+                        size_t workspace_bytes, void *stream);
 
 const char *owq_status_str(owq_status_t s);
 

@@ -18,19 +18,22 @@ LIB_PATH = os.path.join(_HERE, "libowq.so")
 OWQ_OK = 0
 STATUS_NAMES = ["OWQ_OK", "OWQ_ERR_NULL", "OWQ_ERR_SHAPE", "OWQ_ERR_BITS", "OWQ_ERR_GROUP",
                 "OWQ_ERR_CODE_RANGE", "OWQ_ERR_INDEX", "OWQ_ERR_BUFFER", "OWQ_ERR_BATCH",
-                "OWQ_ERR_HANDLE", "OWQ_ERR_HIP", "OWQ_ERR_UNSUPPORTED", "OWQ_ERR_LAYOUT", "OWQ_ERR_SCRATCH"]
+                "OWQ_ERR_HANDLE", "OWQ_ERR_HIP", "OWQ_ERR_UNSUPPORTED", "OWQ_ERR_LAYOUT", "OWQ_ERR_SCRATCH", "OWQ_ERR_TYPE"]
 (OWQ_ERR_NULL, OWQ_ERR_SHAPE, OWQ_ERR_BITS, OWQ_ERR_GROUP, OWQ_ERR_CODE_RANGE, OWQ_ERR_INDEX,
  OWQ_ERR_BUFFER, OWQ_ERR_BATCH, OWQ_ERR_HANDLE, OWQ_ERR_HIP, OWQ_ERR_UNSUPPORTED,
- OWQ_ERR_LAYOUT, OWQ_ERR_SCRATCH) = range(1, 14)
+ OWQ_ERR_LAYOUT, OWQ_ERR_SCRATCH, OWQ_ERR_TYPE) = range(1, 15)
 OWQ_STATIC_SCRATCH_BYTES = 32 << 20
 OWQ_LAYOUT_GEMV, OWQ_LAYOUT_TILE, OWQ_LAYOUT_COMPACT = 0, 1, 2
+OWQ_TYPE_F16, OWQ_TYPE_BF16, OWQ_TYPE_F32 = 0, 1, 2
 
 # every symbol include/owq.h declares
 EXPORTS = ["owq_geometry", "owq_packed_bytes", "owq_pack_host", "owq_unpack_codes", "owq_pack_layer",
            "owq_open_packed", "owq_linear", "owq_free_layer", "owq_layer_info", "owq_export_packed", "owq_set_launch",
            "owq_update_weak", "owq_weak_set_bytes", "owq_pack_weak_set", "owq_linear_multi", "owq_search_config",
            "owq_backward_workspace_bytes", "owq_linear_backward", "owq_probe_read", "owq_probe_read_write", "owq_probe_empty", "owq_probe_alu", "owq_probe_mfma", "owq_workspace_bytes", "owq_linear_ws", "owq_linear_static",
-           "owq_status_str"]
+           "owq_qk_norm_rope", "owq_qk_norm_rope_backward_workspace_bytes", "owq_qk_norm_rope_backward", "owq_cache_page_bytes",
+           "owq_cache_append", "owq_cache_read", "owq_cache_attention_workspace_bytes", "owq_cache_attention",
+           "owq_sample_workspace_bytes", "owq_sample", "owq_status_str"]
 
 
 class OwqError(RuntimeError):
@@ -50,6 +53,22 @@ class LayerDesc(C.Structure):
 class SearchDesc(C.Structure):
     _fields_ = [("d_out", C.c_int32), ("d_in", C.c_int32), ("bits", C.c_int32), ("group_size", C.c_int32),
                 ("k", C.c_int32), ("n_lo", C.c_int32), ("n_hi", C.c_int32), ("shrink", C.c_float)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_tokens", "q_heads", "kv_heads", "head_dim", "rotary_dim", "interleaved", "type",
+                                         "n_positions")] + \
+               [("eps", C.c_float), ("reserved", C.c_int32)] + \
+               [(n, C.c_int64) for n in ("q_token", "q_head", "k_token", "k_head", "dq_token", "dq_head", "dk_token", "dk_head")]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_pages", "page_size", "kv_heads", "head_dim", "n_seqs", "table_stride")]
+
+
+class AttentionDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("q_heads", "type", "n_rows", "max_new", "max_len", "window", "sinks")] + \
+               [("scale", C.c_float), ("q_row", C.c_int64), ("q_head", C.c_int64)]
 
 
 class LayerInfo(C.Structure):
@@ -106,6 +125,18 @@ def lib():
         L.owq_probe_empty.argtypes = [P]
         L.owq_probe_alu.argtypes = [P, C.c_int32, C.c_int32, P]
         L.owq_probe_mfma.argtypes = [P, C.c_int32, C.c_int32, P]
+        I64 = C.c_int64
+        # pointers to descriptions go as void *: the smallest calls pass them as packed bytes
+        L.owq_qk_norm_rope.argtypes = [P] * 11
+        L.owq_qk_norm_rope_backward_workspace_bytes.argtypes = [P, C.POINTER(SZ)]
+        L.owq_qk_norm_rope_backward.argtypes = [P] * 15 + [SZ, P]
+        L.owq_cache_page_bytes.argtypes = [P, C.POINTER(SZ)]
+        L.owq_cache_append.argtypes = [P] * 7 + [I32] * 3 + [I64] * 4 + [P]
+        L.owq_cache_read.argtypes = [P] * 6 + [I32] * 3 + [P]
+        L.owq_cache_attention_workspace_bytes.argtypes = [P, P, C.POINTER(SZ)]
+        L.owq_cache_attention.argtypes = [P] * 10 + [SZ, P]
+        L.owq_sample_workspace_bytes.argtypes = [I32, I32, I32, C.POINTER(SZ)]
+        L.owq_sample.argtypes = [P, I32, I32, I32, I64, P, I64] + [P] * 7 + [SZ, P]
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.owq_status_str.argtypes = [C.c_int]
@@ -337,6 +368,243 @@ def owq_status_str(status: int) -> str:
 def _current_stream(torch) -> int:
     """torch.cuda.current_stream().cuda_stream, which builds two objects for it: 2.7 us against 0.2."""
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+
+
+def owq_qk_norm_rope(desc: RopeDesc, q_ptr, k_ptr, wq_ptr, wk_ptr, cos_ptr, sin_ptr, positions_ptr, q_out_ptr, k_out_ptr,
+                     stream: int = 0) -> None:
+    """Every pointer of this and the following calls is a DEVICE address (0 = NULL where the header allows it)."""
+    _check(lib().owq_qk_norm_rope(C.addressof(desc), q_ptr, k_ptr, wq_ptr, wk_ptr, cos_ptr, sin_ptr, positions_ptr, q_out_ptr,
+                                  k_out_ptr, stream), "owq_qk_norm_rope")
+
+
+def owq_qk_norm_rope_backward_workspace_bytes(desc: RopeDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().owq_qk_norm_rope_backward_workspace_bytes(C.addressof(desc), C.byref(n)), "owq_qk_norm_rope_backward_workspace_bytes")
+    return int(n.value)
+
+
+def owq_qk_norm_rope_backward(desc: RopeDesc, dq_out_ptr, dk_out_ptr, q_ptr, k_ptr, wq_ptr, wk_ptr, cos_ptr, sin_ptr, positions_ptr,
+                              dq_ptr, dk_ptr, dwq_ptr, dwk_ptr, workspace_ptr, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().owq_qk_norm_rope_backward(C.addressof(desc), dq_out_ptr, dk_out_ptr, q_ptr, k_ptr, wq_ptr, wk_ptr, cos_ptr, sin_ptr,
+                                           positions_ptr, dq_ptr, dk_ptr, dwq_ptr, dwk_ptr, workspace_ptr, workspace_bytes, stream),
+           "owq_qk_norm_rope_backward")
+
+
+def owq_cache_page_bytes(desc: CacheDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().owq_cache_page_bytes(C.addressof(desc), C.byref(n)), "owq_cache_page_bytes")
+    return int(n.value)
+
+
+def owq_cache_append(desc: CacheDesc, pages_ptr, table_ptr, starts_ptr, lengths_ptr, k_ptr, v_ptr, type: int, n_rows: int, max_new: int,
+                     k_row: int, k_head: int, v_row: int, v_head: int, stream: int = 0) -> None:
+    _check(lib().owq_cache_append(C.addressof(desc), pages_ptr, table_ptr, starts_ptr, lengths_ptr, k_ptr, v_ptr, type, n_rows, max_new,
+                                  k_row, k_head, v_row, v_head, stream), "owq_cache_append")
+
+
+def owq_cache_read(desc: CacheDesc, pages_ptr, table_ptr, starts_ptr, k_out_ptr, v_out_ptr, type: int, n_rows: int, max_len: int,
+                   stream: int = 0) -> None:
+    _check(lib().owq_cache_read(C.addressof(desc), pages_ptr, table_ptr, starts_ptr, k_out_ptr, v_out_ptr, type, n_rows, max_len, stream),
+           "owq_cache_read")
+
+
+def owq_cache_attention_workspace_bytes(desc: CacheDesc, att: AttentionDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().owq_cache_attention_workspace_bytes(C.addressof(desc), C.addressof(att), C.byref(n)), "owq_cache_attention_workspace_bytes")
+    return int(n.value)
+
+
+def owq_cache_attention(desc: CacheDesc, att: AttentionDesc, q_ptr, pages_ptr, table_ptr, starts_ptr, lengths_ptr, out_ptr, lse_ptr,
+                        workspace_ptr, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().owq_cache_attention(C.addressof(desc), C.addressof(att), q_ptr, pages_ptr, table_ptr, starts_ptr, lengths_ptr, out_ptr,
+                                     lse_ptr, workspace_ptr, workspace_bytes, stream), "owq_cache_attention")
+
+
+def owq_sample_workspace_bytes(n_rows: int, vocab: int, type: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().owq_sample_workspace_bytes(n_rows, vocab, type, C.byref(n)), "owq_sample_workspace_bytes")
+    return int(n.value)
+
+
+def owq_sample(logits_ptr, type: int, n_rows: int, vocab: int, logits_row: int, noise_ptr, noise_row: int, temperature_ptr, top_k_ptr,
+               top_p_ptr, min_p_ptr, token_ptr, logprob_ptr, workspace_ptr, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().owq_sample(logits_ptr, type, n_rows, vocab, logits_row, noise_ptr, noise_row, temperature_ptr, top_k_ptr, top_p_ptr,
+                            min_p_ptr, token_ptr, logprob_ptr, workspace_ptr, workspace_bytes, stream), "owq_sample")
+
+
+_TYPES = None
+
+
+def _type_of(t, f32=False):
+    """OWQ_TYPE_* of a tensor's type."""
+    global _TYPES
+    if _TYPES is None:
+        import torch
+        _TYPES = {torch.float16: OWQ_TYPE_F16, torch.bfloat16: OWQ_TYPE_BF16, torch.float32: OWQ_TYPE_F32}
+    n = _TYPES.get(t.dtype, -1)
+    assert n >= 0 and (f32 or n != OWQ_TYPE_F32), t.dtype
+    return n
+
+
+def _heads(x, what):
+    """[rows, heads, head size] on the GPU, last axis contiguous."""
+    assert x.dim() == 3 and x.is_cuda and (x.stride(2) == 1 or x.shape[2] == 1), (what, x.shape, x.stride())
+    return x
+
+
+def _int32(x, n, what):
+    assert x.is_cuda and x.is_contiguous() and x.numel() >= n and "int32" in str(x.dtype), (what, x.dtype, x.shape)
+    return x.data_ptr()
+
+
+def _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved):
+    import torch
+    _heads(q, "q"), _heads(k, "k")
+    tokens, q_heads, dim = q.shape
+    assert k.shape[0] == tokens and k.shape[2] == dim and k.dtype == q.dtype and k.device == q.device, (q.shape, k.shape)
+    assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
+    assert cos.is_cuda and sin.is_cuda and cos.is_contiguous() and sin.is_contiguous()
+    for w in (wq, wk):
+        assert w is None or (w.dtype == q.dtype and w.is_cuda and w.is_contiguous() and w.numel() == dim)
+    _int32(positions, tokens, "positions")
+    return RopeDesc(tokens, q_heads, k.shape[1], dim, 2 * cos.shape[1], int(interleaved), _type_of(q), cos.shape[0], eps, 0,
+                    q.stride(0), q.stride(1), k.stride(0), k.stride(1), 0, 0, 0, 0)
+
+
+def qk_norm_rope(q, k, cos, sin, positions, wq=None, wk=None, eps=1e-6, interleaved=False, out=None):
+    """owq_qk_norm_rope on CUDA tensors: q [tokens, query heads, head size] and k [tokens, key heads, head size], fp16 or bf16, as
+    slices of one tensor if need be; cos, sin fp32 [positions, rotated columns / 2]; positions int32 [tokens]; wq, wk the norms'
+    weights or None.  Returns (q, k) turned, packed; `out` = a pair of packed tensors to write to (the inputs' own if packed)."""
+    import torch
+    desc = _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved)
+    if out is None:
+        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    else:
+        q_out, k_out = out
+        for o, x in ((q_out, q), (k_out, k)):
+            assert o.shape == x.shape and o.dtype == x.dtype and o.is_cuda and o.is_contiguous()
+    owq_qk_norm_rope(desc, q.data_ptr(), k.data_ptr(), 0 if wq is None else wq.data_ptr(), 0 if wk is None else wk.data_ptr(), cos.data_ptr(),
+                     sin.data_ptr(), positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _current_stream(torch))
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(dq_out, dk_out, q, k, cos, sin, positions, wq=None, wk=None, eps=1e-6, interleaved=False, workspace=None):
+    """owq_qk_norm_rope_backward: gradients of qk_norm_rope's outputs to those of q, k and, fp32, of the weights (None without one).
+    q, k: the forward's inputs (read only where there is a weight).  Returns (dq, dk, dwq, dwk)."""
+    import torch
+    desc = _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved)
+    for d, x in ((dq_out, q), (dk_out, k)):
+        assert _heads(d, "gradient").shape == x.shape and d.dtype == x.dtype
+    desc.dq_token, desc.dq_head, desc.dk_token, desc.dk_head = dq_out.stride(0), dq_out.stride(1), dk_out.stride(0), dk_out.stride(1)
+    dev = q.device
+    dq, dk = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
+    dwq = None if wq is None else torch.empty(q.shape[2], dtype=torch.float32, device=dev)
+    dwk = None if wk is None else torch.empty(q.shape[2], dtype=torch.float32, device=dev)
+    if workspace is None and (dwq is not None or dwk is not None):
+        workspace = torch.empty(max(16, owq_qk_norm_rope_backward_workspace_bytes(desc)), dtype=torch.uint8, device=dev)
+    owq_qk_norm_rope_backward(desc, dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), 0 if wq is None else wq.data_ptr(),
+                              0 if wk is None else wk.data_ptr(), cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), dq.data_ptr(),
+                              dk.data_ptr(), 0 if dwq is None else dwq.data_ptr(), 0 if dwk is None else dwk.data_ptr(),
+                              0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
+                              _current_stream(torch))
+    return dq, dk, dwq, dwk
+
+
+def cache_empty(n_pages, page_size, kv_heads, head_dim, device="cuda"):
+    """Pages for the 4-bit cache: uint8 [n_pages, kv_heads, page_size / 32, bytes of a tile], contents undefined."""
+    import torch
+    n = owq_cache_page_bytes(CacheDesc(1, page_size, kv_heads, head_dim, 0, 0))
+    tiles = page_size // 32
+    return torch.empty((n_pages, kv_heads, tiles, n // (kv_heads * tiles)), dtype=torch.uint8, device=device)
+
+
+def _cache_desc(pages, table, n_seqs, kv_heads, dim):
+    assert pages.dim() == 4 and pages.is_cuda and pages.is_contiguous() and pages.element_size() == 1, pages.shape
+    assert table.dim() == 2 and table.shape[0] >= n_seqs
+    _int32(table, 1, "page_table")
+    n_pages, heads, tiles, size = pages.shape
+    assert heads == kv_heads and size == 32 * ((dim + 31) // 32 * 32) + 256, (pages.shape, kv_heads, dim)
+    return CacheDesc(n_pages, 32 * tiles, heads, dim, n_seqs, table.shape[1])
+
+
+def cache_append(pages, page_table, starts, lengths, k, v, max_new=None):
+    """owq_cache_append: rows of k and v [rows, key/value heads, head size] into the pages.  page_table int32 [sequences, pages];
+    starts int32 [sequences + 1], the rows of each sequence; lengths int32 [sequences], its tokens with the new ones.
+    max_new: the most rows of a sequence (default: all rows; a smaller bound spares empty workgroups)."""
+    import torch
+    _heads(k, "k"), _heads(v, "v")
+    assert k.shape == v.shape and k.dtype == v.dtype
+    n_seqs = lengths.numel()
+    rows, heads, dim = k.shape
+    desc = _cache_desc(pages, page_table, n_seqs, heads, dim)
+    owq_cache_append(desc, pages.data_ptr(), page_table.data_ptr(), _int32(starts, n_seqs + 1, "starts"), _int32(lengths, n_seqs, "lengths"),
+                     k.data_ptr(), v.data_ptr(), _type_of(k), rows, rows if max_new is None else max_new, k.stride(0), k.stride(1),
+                     v.stride(0), v.stride(1), _current_stream(torch))
+
+
+def cache_read(pages, page_table, starts, n_rows, head_dim, max_len=None, dtype=None):
+    """owq_cache_read: tokens 0 .. starts[b + 1] - starts[b] - 1 of every sequence as (k, v) [n_rows, key/value heads, head_dim]."""
+    import torch
+    n_seqs = starts.numel() - 1
+    desc = _cache_desc(pages, page_table, n_seqs, pages.shape[1], head_dim)
+    _int32(starts, n_seqs + 1, "starts")
+    shape = (n_rows, pages.shape[1], head_dim)
+    dtype = torch.float16 if dtype is None else dtype
+    k, v = torch.empty(shape, dtype=dtype, device=pages.device), torch.empty(shape, dtype=dtype, device=pages.device)
+    owq_cache_read(desc, pages.data_ptr(), page_table.data_ptr(), starts.data_ptr(), k.data_ptr(), v.data_ptr(), _type_of(k), n_rows,
+                   n_rows if max_len is None else max_len, _current_stream(torch))
+    return k, v
+
+
+def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0, sinks=0, max_new=None, max_len=None, out=None,
+                    want_lse=False, workspace=None):
+    """owq_cache_attention: q [rows, query heads, head size], fp16 or bf16, over the pages; starts, lengths, page_table as for
+    cache_append.  scale: 1 / sqrt(head size) if None.  max_new, max_len: the most rows and tokens of a sequence (defaults: all rows,
+    the table's capacity; the work is split by these bounds).  Returns out, or (out, lse)."""
+    import torch
+    _heads(q, "q")
+    rows, q_heads, dim = q.shape
+    n_seqs = lengths.numel()
+    desc = _cache_desc(pages, page_table, n_seqs, pages.shape[1], dim)
+    if out is None:
+        out = torch.empty((rows, q_heads, dim), dtype=q.dtype, device=q.device)
+    else:
+        assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.is_contiguous()
+    lse = torch.empty((rows, q_heads), dtype=torch.float32, device=q.device) if want_lse else None
+    most = desc.table_stride * desc.page_size
+    att = AttentionDesc(q_heads, _type_of(q), rows, rows if max_new is None else max_new, most if max_len is None else min(max_len, most),
+                        window, sinks, dim ** -0.5 if scale is None else scale, q.stride(0), q.stride(1))
+    if workspace is None:
+        n = owq_cache_attention_workspace_bytes(desc, att)
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    owq_cache_attention(desc, att, q.data_ptr(), pages.data_ptr(), page_table.data_ptr(), _int32(starts, n_seqs + 1, "starts"),
+                        _int32(lengths, n_seqs, "lengths"), out.data_ptr(), lse.data_ptr() if want_lse else 0,
+                        workspace.data_ptr() if workspace is not None else 0, workspace.numel() if workspace is not None else 0,
+                        _current_stream(torch))
+    return (out, lse) if want_lse else out
+
+
+def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
+    """owq_sample: logits [rows, vocabulary] (fp16, bf16 or fp32), noise fp32 [rows, vocabulary] exponential variates (None if every
+    temperature is 0); temperature, top_p, min_p fp32 and top_k int32 [rows] or None.  Returns (token int32, log-probability fp32)."""
+    import torch
+    assert logits.dim() == 2 and logits.is_cuda and (logits.stride(1) == 1 or logits.shape[1] == 1)
+    rows, vocab = logits.shape
+    if noise is not None:
+        assert noise.dtype == torch.float32 and noise.shape == logits.shape and noise.is_cuda and (noise.stride(1) == 1 or vocab == 1)
+    for x in (temperature, top_p, min_p):
+        assert x is None or (x.dtype == torch.float32 and x.is_cuda and x.is_contiguous() and x.numel() == rows)
+    if top_k is not None:
+        _int32(top_k, rows, "top_k")
+    kind = _type_of(logits, f32=True)
+    token = torch.empty(rows, dtype=torch.int32, device=logits.device)
+    logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
+    n = owq_sample_workspace_bytes(rows, vocab, kind)
+    workspace = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
+    ptr = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
+    owq_sample(logits.data_ptr(), kind, rows, vocab, logits.stride(0), ptr(noise), 0 if noise is None else noise.stride(0), ptr(temperature),
+               ptr(top_k), ptr(top_p), ptr(min_p), token.data_ptr(), logprob.data_ptr(), ptr(workspace), n, _current_stream(torch))
+    return token, logprob
 
 
 class OwqLinear:

@@ -353,6 +353,7 @@ const char *owq_status_str(owq_status_t s) {
     case OWQ_ERR_UNSUPPORTED: return "layer too large for one workgroup's on-chip memory";
     case OWQ_ERR_LAYOUT: return "unknown layout";
     case OWQ_ERR_SCRATCH: return "the layer needs more scratch memory than the library's static array holds";
+    case OWQ_ERR_TYPE: return "unknown or unsupported type";
   }
   return "unknown status";
 }

@@ -1,0 +1,214 @@
+// The cache of keys and values in 4 bits: new rows into it, and its contents back as fp16 or bf16.
+// Layout and rounding: include/owq.h.
+//
+// A workgroup takes 32 tokens of one head (a tile).  Codes go through LDS as bytes [token][column]:
+// rows of the cache's matrix-core words are gathered there (keys: 8 columns of a token, values: 8
+// tokens of a column), so that both sides of the exchange are whole 16- and 8-byte accesses.
+#include <hip/hip_runtime.h>
+
+#include "owq_cache_device.h"
+#include "owq_step.h"
+#include "owq_step_device.h"
+
+namespace owq {
+
+CacheView cache_view(const owq_cache_desc_t &d, const void *pages, const int32_t *table, const int32_t *starts,
+                     const int32_t *lengths, int32_t n_rows) {
+  CacheView c;
+  c.pages = static_cast<uint8_t *>(const_cast<void *>(pages));
+  c.table = table;
+  c.starts = starts;
+  c.lengths = lengths;
+  c.tile_bytes = 32 * ((d.head_dim + 31) / 32 * 32) + 256;
+  c.page_bytes = (int64_t)c.tile_bytes * (d.page_size / 32) * d.kv_heads;
+  c.n_pages = d.n_pages;
+  c.page_shift = 0;
+  while ((32 << c.page_shift) < d.page_size) ++c.page_shift;
+  c.kv_heads = d.kv_heads;
+  c.head_dim = d.head_dim;
+  c.table_stride = d.table_stride;
+  c.n_seqs = d.n_seqs;
+  c.n_rows = n_rows;
+  return c;
+}
+
+// Codes of a row's 16 columns held by one of its 8 threads.  Returns (s, lo) as an fp16 pair.
+template <class E>
+__device__ __forceinline__ u32 quantise(u32x4 a, u32x4 b, bool on0, bool on1, u32 *codes) {
+  float f[16];
+  unpack8<E>(a, f);
+  unpack8<E>(b, f + 8);
+  float hi = -__builtin_inff(), lo = __builtin_inff(), bad = 0.f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const bool on = j < 8 ? on0 : on1;
+    hi = on ? fmaxf(hi, f[j]) : hi;
+    lo = on ? fminf(lo, f[j]) : lo;
+    bad = on && !(__builtin_fabsf(f[j]) < __builtin_inff()) ? 1.f : bad;
+  }
+  hi = lanes_max<8>(hi);
+  lo = -lanes_max<8>(-lo);
+  bad = lanes_max<8>(bad);
+  const float third = 1.0f / 15.0f;
+  const _Float16 s16 = (_Float16)fminf(fmaxf((hi - lo) * third, 0x1p-24f), 65504.f);
+  const _Float16 l16 = (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f);
+  const float s = (float)s16, l = (float)l16;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u32 w = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float q = fminf(fmaxf(__builtin_rintf((f[4 * i + j] - l) / s), 0.f), 15.f);
+      w |= (u32)(int)q << (8 * j);
+    }
+    codes[i] = (bad != 0.f || (i < 2 ? !on0 : !on1)) ? 0u : w;
+  }
+  const h2_t pair = {s16, l16};
+  return bad != 0.f ? 0x7e007e00u : __builtin_bit_cast(u32, pair);
+}
+
+struct AppendArgs {
+  CacheView c;
+  const u32 *k, *v;
+  int64_t k_row, k_head, v_row, v_head;
+};
+
+constexpr int kCodePitch = 136;   // bytes of a token's codes in LDS: 128 columns, 8-byte units on other banks
+
+template <class E>
+__global__ __launch_bounds__(256) void owq_cache_append_kernel(AppendArgs a) {
+  __shared__ __align__(16) uint8_t codes[2][32 * kCodePitch];
+  const CacheView &c = a.c;
+  const int b = blockIdx.z, head = blockIdx.y;
+  const int row0 = c.starts[b], n_new = c.starts[b + 1] - row0, len = c.lengths[b];
+  const int first = len - n_new, from = first < 0 ? 0 : first;     // position of row 0, first position written
+  if (n_new <= 0 || len <= from) return;
+  const int tile = from / 32 + (int)blockIdx.x;
+  const int t0 = from > tile * 32 ? from - tile * 32 : 0;
+  const int t1 = len - tile * 32 < 32 ? len - tile * 32 : 32;       // tokens [t0, t1) of the tile are new
+  if (t1 <= t0) return;
+  uint8_t *dst = cache_tile(c, b, head, tile);
+  if (dst == nullptr) return;
+  const int pad = (c.head_dim + 31) / 32 * 32;
+
+  // rows in: thread = (token, 16 columns)
+  const int token = threadIdx.x >> 3, col = (threadIdx.x & 7) * 16;
+  const int64_t row = (int64_t)row0 + tile * 32 + token - first;
+  const bool on = token >= t0 && token < t1 && row >= 0 && row < c.n_rows;
+  const bool on0 = on && col < c.head_dim, on1 = on && col + 8 < c.head_dim;
+  const u32x4 zero = {0, 0, 0, 0};
+  const u32 *kr = a.k + (row * a.k_row + head * a.k_head + col) / 2, *vr = a.v + (row * a.v_row + head * a.v_head + col) / 2;
+  const u32x4 k0 = on0 ? *reinterpret_cast<const u32x4 *>(kr) : zero, k1 = on1 ? *reinterpret_cast<const u32x4 *>(kr + 4) : zero;
+  const u32x4 v0 = on0 ? *reinterpret_cast<const u32x4 *>(vr) : zero, v1 = on1 ? *reinterpret_cast<const u32x4 *>(vr + 4) : zero;
+  u32 w[4];
+  const u32 km = quantise<E>(k0, k1, on0, on1, w);
+  if (col < pad) *reinterpret_cast<u32x4 *>(&codes[0][token * kCodePitch + col]) = (u32x4){w[0], w[1], w[2], w[3]};
+  const u32 vm = quantise<E>(v0, v1, on0, on1, w);
+  if (col < pad) *reinterpret_cast<u32x4 *>(&codes[1][token * kCodePitch + col]) = (u32x4){w[0], w[1], w[2], w[3]};
+  if (on && col == 0) {
+    u32 *meta = reinterpret_cast<u32 *>(dst + 32 * pad);
+    meta[token] = km;
+    meta[32 + token] = vm;
+  }
+  __syncthreads();
+
+  // words out: thread = (32 columns S, quad q, r), two words of keys and two of values
+  const int i = threadIdx.x;
+  if (i >= 2 * pad) return;
+  const int r = i & 15, q = (i >> 4) & 3, S = i >> 6;
+  u32 *kw = reinterpret_cast<u32 *>(dst) + 2 * i, *vw = reinterpret_cast<u32 *>(dst + 16 * pad) + 2 * i;
+  // rows that lie outside the caller's tensors are not written
+  auto fresh = [&](int t) {
+    const int64_t x = (int64_t)row0 + tile * 32 + t - first;
+    return t >= t0 && t < t1 && x < c.n_rows && x >= 0;
+  };
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int t = 16 * h + r;
+    const u32x2 p = *reinterpret_cast<const u32x2 *>(&codes[0][t * kCodePitch + 32 * S + 8 * q]);
+    if (fresh(t)) kw[h] = word_of_bytes(p.x, p.y);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    u32 word = 0, mask = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = 16 * (e >> 2) + 4 * q + (e & 3);
+      const int at = 4 * ((e >> 1) + 4 * (e & 1));
+      const bool in = fresh(t);
+      word |= in ? (u32)codes[1][t * kCodePitch + 32 * S + 16 * j + r] << at : 0u;
+      mask |= in ? 15u << at : 0u;
+    }
+    if (mask == 0xffffffffu) vw[j] = word;
+    else if (mask != 0) vw[j] = (vw[j] & ~mask) | word;
+  }
+}
+
+struct ReadArgs {
+  CacheView c;
+  u32 *k_out, *v_out;
+};
+
+template <class E>
+__global__ __launch_bounds__(256) void owq_cache_read_kernel(ReadArgs a) {
+  __shared__ __align__(16) uint8_t codes[2][32 * kCodePitch];
+  const CacheView &c = a.c;
+  const int b = blockIdx.z, head = blockIdx.y, tile = blockIdx.x;
+  const int64_t row0 = c.starts[b];
+  const int64_t n = c.starts[b + 1] - row0 - (int64_t)tile * 32;    // tokens wanted from this tile on
+  if (n <= 0) return;
+  const uint8_t *src = cache_tile(c, b, head, tile);
+  const int pad = (c.head_dim + 31) / 32 * 32;
+  const int i = threadIdx.x, r = i & 15, q = (i >> 4) & 3, S = i >> 6;
+  if (src != nullptr && i < 2 * pad) {
+    const u32x2 kw = reinterpret_cast<const u32x2 *>(src)[i], vw = reinterpret_cast<const u32x2 *>(src + 16 * pad)[i];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      *reinterpret_cast<u32x2 *>(&codes[0][(16 * h + r) * kCodePitch + 32 * S + 8 * q]) = bytes_of_word(kw[h]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        codes[1][(16 * (e >> 2) + 4 * q + (e & 3)) * kCodePitch + 32 * S + 16 * j + r] = (vw[j] >> (4 * ((e >> 1) + 4 * (e & 1)))) & 15u;
+  }
+  __syncthreads();
+  const int token = threadIdx.x >> 3, col = (threadIdx.x & 7) * 16;
+  const int64_t row = row0 + (int64_t)tile * 32 + token;
+  if (token >= n || row < 0 || row >= c.n_rows) return;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const u32 m = src ? reinterpret_cast<const u32 *>(src + 32 * pad)[32 * x + token] : 0u;
+    const float s = half_lo(m), lo = half_hi(m);
+    u32 *out = (x ? a.v_out : a.k_out) + (row * c.kv_heads + head) * (c.head_dim / 2);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int at = col + 8 * half;
+      if (at >= c.head_dim) continue;
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = src ? __builtin_fmaf(s, (float)codes[x][token * kCodePitch + at + j], lo) : 0.f;
+      *reinterpret_cast<u32x4 *>(out + at / 2) = pack8<E>(f);
+    }
+  }
+}
+
+int launch_cache_append(const CacheView &c, const void *k, const void *v, int32_t type, int32_t max_new, int64_t k_row,
+                        int64_t k_head, int64_t v_row, int64_t v_head, void *stream) {
+  const AppendArgs a{c, static_cast<const u32 *>(k), static_cast<const u32 *>(v), k_row, k_head, v_row, v_head};
+  // max_new tokens touch at most this many tiles, wherever the first of them lies
+  const dim3 grid((unsigned)((max_new + 30) / 32 + 1), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  if (type == OWQ_TYPE_F16) owq_cache_append_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  else owq_cache_append_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  return (int)hipGetLastError();
+}
+
+int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type, int32_t max_len, void *stream) {
+  const ReadArgs a{c, static_cast<u32 *>(k_out), static_cast<u32 *>(v_out)};
+  const dim3 grid((unsigned)((max_len + 31) / 32), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  if (type == OWQ_TYPE_F16) owq_cache_read_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  else owq_cache_read_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+  return (int)hipGetLastError();
+}
+
+}  // namespace owq

@@ -1,0 +1,71 @@
+// Device-side helpers of the operators between two layers: 16-byte pieces of fp16 or bf16 rows
+// as eight floats and back, sums over a few neighbouring lanes.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "owq_device.h"
+
+namespace owq {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+
+struct F16 {
+  static __device__ __forceinline__ float lo(u32 w) { return half_lo(w); }
+  static __device__ __forceinline__ float hi(u32 w) { return half_hi(w); }
+  static __device__ __forceinline__ u32 pack(float a, float b) {
+    const h2_t h = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(u32, h);
+  }
+};
+
+struct BF16 {
+  static __device__ __forceinline__ float lo(u32 w) { return __builtin_bit_cast(float, w << 16); }
+  static __device__ __forceinline__ float hi(u32 w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+  static __device__ __forceinline__ u32 pack(float a, float b) {
+    typedef __bf16 b2_t __attribute__((ext_vector_type(2)));
+    const b2_t h = {(__bf16)a, (__bf16)b};       // to nearest, ties to even, NaN stays NaN
+    return __builtin_bit_cast(u32, h);
+  }
+};
+
+template <class E>
+__device__ __forceinline__ void unpack8(u32x4 v, float *f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = E::lo(v[i]);
+    f[2 * i + 1] = E::hi(v[i]);
+  }
+}
+
+template <class E>
+__device__ __forceinline__ u32x4 pack8(const float *f) {
+  return (u32x4){E::pack(f[0], f[1]), E::pack(f[2], f[3]), E::pack(f[4], f[5]), E::pack(f[6], f[7])};
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+
+// Sum over L = 1, 2, 4, 8 or 16 neighbouring lanes (every lane gets the total), in a fixed order.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if (L >= 2) v += dpp<0xB1>(v);     // lanes ^1
+  if (L >= 4) v += dpp<0x4E>(v);     // lanes ^2
+  if (L >= 8) v += dpp<0x141>(v);    // mirror in 8
+  if (L >= 16) v += dpp<0x140>(v);   // mirror in 16
+  return v;
+}
+
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  if (L >= 2) v = fmaxf(v, dpp<0xB1>(v));
+  if (L >= 4) v = fmaxf(v, dpp<0x4E>(v));
+  if (L >= 8) v = fmaxf(v, dpp<0x141>(v));
+  if (L >= 16) v = fmaxf(v, dpp<0x140>(v));
+  return v;
+}
+
+}  // namespace owq

@@ -405,7 +405,8 @@ owq_status_t owq_linear_backward(owq_handle_t h, const void *dy, const void *x, 
  * NULL has none).  With g the gradient turned back, r = 1 / sqrt(mean(x^2) + eps), h = g w:
  *     dw = sum g x r,   dx = r (h - x r^2 mean(h x))          (dx = g without a weight)
  * workspace: owq_qk_norm_rope_backward_workspace_bytes bytes, 16-byte aligned, contents
- * undefined before and after (may be NULL if the answer is 0: no weight, or no gradient of one wanted).
+ * undefined before and after (may be NULL if it is 0 bytes or no weight's gradient is wanted).  Without
+ * tokens the weights' gradients are 0.
  */
 typedef struct {
   int32_t n_tokens, q_heads, kv_heads, head_dim, rotary_dim;

@@ -11,8 +11,10 @@
 // taken 16 times as large to even that out, the rest is undone in fp32: with q' = q 2^k of a row whose
 // largest element lies in [2^10, 2^11), sum c q = acc 2^(20 - k), and
 //     y = s (sum c q) + lo (sum q)      (times scale log2 e)
-// The values' least parts need no product: out = sum (p s) c + sum p lo, the second sum one number
-// per row.
+// The values' least parts need no product, and the weights' rounding to fp16 should act on codes
+// measured from their middle: out = sum w (c - 8) + sum p (lo + 8 s) with w the rounded p s; the second
+// sum is one number per row, and sum w 8 the product with a word of codes 8 (without it the rounding of
+// weights errs on c in 0..15, and on values of mean 0 almost three times as far).
 //
 // Softmax with a running reference: weights are p = 2^(y - ref), and ref is raised (sums and products
 // so far scaled down) only where some p s would leave fp16's range, above 2^11; it begins so low that
@@ -112,7 +114,7 @@ struct Rows {
   float c1[NQ], x1[NQ];           // factors of s acc and of lo
   float ref[NQ], l[NQ], low[NQ];  // reference, sum of p, sum of p lo (of this lane's keys)
   int pos[NQ];
-  f32x4 acc[NQ][2 * STEPS];
+  f32x4 acc[NQ][2 * STEPS], mid[NQ];   // sums of w c 2^-20, and of w 8 2^-20 in every register
 };
 
 __device__ __forceinline__ bool sees(int key, int pos, int window, int sinks) {
@@ -174,6 +176,7 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, const Tile<STEP
       w.low[n] *= alpha;
 #pragma unroll
       for (int d = 0; d < 2 * STEPS; ++d) w.acc[n][d] *= alpha;
+      w.mid[n] *= alpha;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bool on = (seen >> i) & 1u;
@@ -185,11 +188,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, const Tile<STEP
     for (int i = 0; i < 8; ++i) {
       w.l[n] += p[i];
       const float lo = half_hi(t.vm[i >> 2][i & 3]);
-      w.low[n] = __builtin_fmaf(p[i], edge ? ((seen >> i) & 1u ? lo : 0.f) : lo, w.low[n]);
+      w.low[n] = __builtin_fmaf(p[i], edge ? ((seen >> i) & 1u ? lo : 0.f) : lo, __builtin_fmaf(8.f, pv[i], w.low[n]));
     }
     const u32x4 b = {F16::pack(16.f * pv[0], 16.f * pv[1]), F16::pack(pv[2], pv[3]), F16::pack(16.f * pv[4], 16.f * pv[5]),
                      F16::pack(pv[6], pv[7])};
     pb[n] = __builtin_bit_cast(h8_t, b);
+    w.mid[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(0x88888888u), pb[n], w.mid[n], 0, 0, 0);
   }
 #pragma unroll
   for (int st = 0; st < STEPS; ++st)
@@ -271,6 +275,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kerne
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < 2 * STEPS; ++d) w.acc[n][d] = zero;
+    w.mid[n] = zero;
   }
 
   // tiles of this wave: all of the range, or every kWaves-th
@@ -315,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kerne
           if (dim >= c.head_dim) continue;
           float o[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r], 0x1p20f, low) * inv;
+          for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r] - w.mid[n][r], 0x1p20f, low) * inv;
           const u32x2 packed = a.bf16 ? (u32x2){BF16::pack(o[0], o[1]), BF16::pack(o[2], o[3])} : (u32x2){F16::pack(o[0], o[1]), F16::pack(o[2], o[3])};
           *reinterpret_cast<u32x2 *>(out + dim / 2) = packed;
         }
@@ -328,7 +333,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kerne
     for (int d = 0; d < 2 * STEPS; ++d) {
       f32x4 o;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r], 0x1p20f, low);
+      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r] - w.mid[n][r], 0x1p20f, low);
       *reinterpret_cast<f32x4 *>(&red[wave][col][16 * d + 4 * quad]) = o;
     }
     if (quad == 0) {

@@ -187,7 +187,10 @@ __global__ __launch_bounds__(256) void owq_cache_read_kernel(ReadArgs a) {
       if (at >= c.head_dim) continue;
       float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = src ? __builtin_fmaf(s, (float)codes[x][token * kCodePitch + at + j], lo) : 0.f;
+      for (int j = 0; j < 8; ++j) {
+        f[j] = src ? __builtin_fmaf(s, (float)codes[x][token * kCodePitch + at + j], lo) : 0.f;
+        asm("" : "+v"(f[j]));      // a binary32 value: not to be fused with the rounding to 16 bits
+      }
       *reinterpret_cast<u32x4 *>(out + at / 2) = pack8<E>(f);
     }
   }

@@ -290,13 +290,13 @@ int launch_rope_backward(const owq_rope_desc_t &d, const RopePtrs &p, void *stre
   const RopeArgs a = rope_args(d, p);
   const int lanes = rope_lanes(d), threads = rope_threads(d, lanes);
   const int blocks = rope_backward_blocks(d);
-  for_kinds(d.type, d.interleaved != 0, [&](auto e, auto inter) {
+  if (blocks > 0) for_kinds(d.type, d.interleaved != 0, [&](auto e, auto inter) {
     for_lanes(lanes, [&](auto l) {
       owq_rope_backward_kernel<decltype(e), decltype(inter)::value, decltype(l)::value>
           <<<blocks, threads, 0, static_cast<hipStream_t>(stream)>>>(a);
     });
   });
-  if (a.partial != nullptr)
+  if (p.dwq != nullptr || p.dwk != nullptr)      // no tokens: zeros
     owq_rope_weights_kernel<<<(2 * d.head_dim + 31) / 32, 1024, 0, static_cast<hipStream_t>(stream)>>>(a.partial, blocks, d.head_dim, p.dwq, p.dwk);
   return (int)hipGetLastError();
 }

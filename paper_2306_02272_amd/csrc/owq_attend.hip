@@ -76,30 +76,32 @@ __device__ __forceinline__ Span visible_tiles(const AttendArgs &a, int pa, int p
   return s;
 }
 
+// A tile's words and pairs as one lane holds them: keys 16 h + 4 quad + r in km[h][r], vm[h][r].
 template <int STEPS>
 struct Tile {
   u32x2 k[STEPS], v[STEPS];
   u32x4 km[2], vm[2];
-  int key0;           // first key
-  bool there;
 };
 
 template <int STEPS>
-__device__ __forceinline__ void load_tile(const CacheView &c, int b, int head, int tile, int lane, Tile<STEPS> &t) {
-  const uint8_t *p = cache_tile(c, b, head, tile);
-  t.there = p != nullptr;
-  t.key0 = tile * 32;
-  p = t.there ? p : c.pages;             // some page, all of it masked
-  const u32x2 *w = reinterpret_cast<const u32x2 *>(p) + lane;
+__device__ __forceinline__ void load_keys(const uint8_t *p, u32 lane8, Tile<STEPS> &t) {
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) t.k[s] = w[64 * s];
-  const u32x4 *m = reinterpret_cast<const u32x4 *>(p + 1024 * STEPS) + (lane >> 4);
+  for (int s = 0; s < STEPS; ++s) t.k[s] = *reinterpret_cast<const u32x2 *>(p + lane8 + 512 * s);
+}
+
+template <int STEPS>
+__device__ __forceinline__ void load_values(const uint8_t *p, u32 lane8, Tile<STEPS> &t) {
 #pragma unroll
-  for (int h = 0; h < 2; ++h) t.km[h] = m[4 * h];
+  for (int s = 0; s < STEPS; ++s) t.v[s] = *reinterpret_cast<const u32x2 *>(p + lane8 + 512 * (STEPS + s));
+}
+
+template <int STEPS>
+__device__ __forceinline__ void load_pairs(const uint8_t *p, u32 quad16, Tile<STEPS> &t) {
 #pragma unroll
-  for (int s = 0; s < STEPS; ++s) t.v[s] = w[64 * (STEPS + s)];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) t.vm[h] = m[8 + 4 * h];
+  for (int h = 0; h < 2; ++h) {
+    t.km[h] = *reinterpret_cast<const u32x4 *>(p + quad16 + 1024 * STEPS + 64 * h);
+    t.vm[h] = *reinterpret_cast<const u32x4 *>(p + quad16 + 1024 * STEPS + 128 + 64 * h);
+  }
 }
 
 // The eight codes of a word as fp16 numbers: c 2^-24 at elements 0, 1, 4, 5, c 2^-20 at the others.
@@ -112,21 +114,77 @@ template <int STEPS, int NQ>
 struct Rows {
   h8_t q[NQ][STEPS];
   float c1[NQ], x1[NQ];           // factors of s acc and of lo
-  float ref[NQ], l[NQ], low[NQ];  // reference, sum of p, sum of p lo (of this lane's keys)
+  float ref[NQ], l[NQ], low[NQ];  // reference, sum of p, sum of p (lo + 8 s), of this lane's keys
   int pos[NQ];
   f32x4 acc[NQ][2 * STEPS], mid[NQ];   // sums of w c 2^-20, and of w 8 2^-20 in every register
 };
 
-__device__ __forceinline__ bool sees(int key, int pos, int window, int sinks) {
-  return key <= pos && (window == 0 || key > pos - window || key < sinks);
+// Scores to weights for one column tile: s = the products of this lane's eight keys, EDGE: some of them are masked, those
+// with index (16 h + r) above `hi`, and those not above `lo` unless below `sink`.
+template <bool EDGE, int STEPS, int NQ>
+__device__ __forceinline__ h8_t weights(const f32x4 (&s)[2], const Tile<STEPS> &t, int hi, int lo, int sink, int n,
+                                        Rows<STEPS, NQ> &w) {
+  float p[8], pv[8], most = 0.f;
+  bool on[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int at = 16 * (i >> 2) + (i & 3);
+    on[i] = !EDGE || (at <= hi && (at > lo || at < sink));
+    const u32 km = t.km[i >> 2][i & 3], vm = t.vm[i >> 2][i & 3];
+    const float y = __builtin_fmaf(half_lo(km), s[i >> 2][i & 3] * w.c1[n], __builtin_fmaf(half_hi(km), w.x1[n], -w.ref[n]));
+    p[i] = __builtin_amdgcn_exp2f(y);
+    pv[i] = p[i] * half_lo(vm);
+    if (EDGE) {
+      p[i] = on[i] ? p[i] : 0.f;
+      pv[i] = on[i] ? pv[i] : 0.f;
+    }
+    most = fmaxf(most, pv[i]);
+  }
+  if (__any(most > kLimit)) {
+    float y[8], top = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const u32 km = t.km[i >> 2][i & 3], vm = t.vm[i >> 2][i & 3];
+      y[i] = __builtin_fmaf(half_lo(km), s[i >> 2][i & 3] * w.c1[n], half_hi(km) * w.x1[n]);
+      const float z = fmaxf(top, y[i] + __builtin_amdgcn_logf(half_lo(vm)));
+      top = on[i] ? z : top;
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float ref = fmaxf(w.ref[n], top);
+    const float alpha = __builtin_amdgcn_exp2f(w.ref[n] - ref);
+    w.ref[n] = ref;
+    w.l[n] *= alpha;
+    w.low[n] *= alpha;
+#pragma unroll
+    for (int d = 0; d < 2 * STEPS; ++d) w.acc[n][d] *= alpha;
+    w.mid[n] *= alpha;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(y[i] - ref);
+      pv[i] = p[i] * half_lo(t.vm[i >> 2][i & 3]);
+      if (EDGE) {
+        p[i] = on[i] ? p[i] : 0.f;
+        pv[i] = on[i] ? pv[i] : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    w.l[n] += p[i];
+    const u32 vm = t.vm[i >> 2][i & 3];
+    const float lo8 = __builtin_fmaf(8.f, half_lo(vm), half_hi(vm));
+    w.low[n] = __builtin_fmaf(p[i], EDGE ? (on[i] ? lo8 : 0.f) : lo8, w.low[n]);
+  }
+  const u32x4 b = {F16::pack(16.f * pv[0], 16.f * pv[1]), F16::pack(pv[2], pv[3]), F16::pack(16.f * pv[4], 16.f * pv[5]),
+                   F16::pack(pv[6], pv[7])};
+  return __builtin_bit_cast(h8_t, b);
 }
 
 template <int STEPS, int NQ>
-__device__ __forceinline__ void attend_tile(const AttendArgs &a, const Tile<STEPS> &t, int lane, bool edge, Rows<STEPS, NQ> &w) {
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4 s[NQ][2];
+__device__ __forceinline__ void scores(const Tile<STEPS> &t, const Rows<STEPS, NQ> &w, f32x4 (&s)[NQ][2]) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) s[n][0] = s[n][1] = zero;
+  for (int n = 0; n < NQ; ++n) s[n][0] = s[n][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int st = 0; st < STEPS; ++st)
 #pragma unroll
@@ -135,66 +193,12 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, const Tile<STEP
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, w.q[n][st], s[n][h], 0, 0, 0);
     }
-  h8_t pb[NQ];
+}
+
+template <int STEPS, int NQ>
+__device__ __forceinline__ void products(const Tile<STEPS> &t, const h8_t (&pb)[NQ], Rows<STEPS, NQ> &w) {
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    float p[8], pv[8], most = 0.f;
-    u32 seen = 0xffu;
-    if (edge) {
-      seen = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = t.key0 + 16 * (i >> 2) + 4 * (lane >> 4) + (i & 3);
-        seen |= (t.there && key < a.max_len && sees(key, w.pos[n], a.window, a.sinks)) ? 1u << i : 0u;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const u32 km = t.km[i >> 2][i & 3], vm = t.vm[i >> 2][i & 3];
-      const float y = __builtin_fmaf(half_lo(km), s[n][i >> 2][i & 3] * w.c1[n], __builtin_fmaf(half_hi(km), w.x1[n], -w.ref[n]));
-      p[i] = __builtin_amdgcn_exp2f(y);
-      pv[i] = p[i] * half_lo(vm);
-      if (edge && !((seen >> i) & 1u)) p[i] = pv[i] = 0.f;
-      most = fmaxf(most, pv[i]);
-    }
-    if (__any(most > kLimit)) {
-      float top = -__builtin_inff();
-      float y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const u32 km = t.km[i >> 2][i & 3], vm = t.vm[i >> 2][i & 3];
-        y[i] = __builtin_fmaf(half_lo(km), s[n][i >> 2][i & 3] * w.c1[n], half_hi(km) * w.x1[n]);
-        const float z = y[i] + __builtin_amdgcn_logf(half_lo(vm));
-        top = (seen >> i) & 1u ? fmaxf(top, z) : top;
-      }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float ref = fmaxf(w.ref[n], top);
-      const float alpha = __builtin_amdgcn_exp2f(w.ref[n] - ref);
-      w.ref[n] = ref;
-      w.l[n] *= alpha;
-      w.low[n] *= alpha;
-#pragma unroll
-      for (int d = 0; d < 2 * STEPS; ++d) w.acc[n][d] *= alpha;
-      w.mid[n] *= alpha;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool on = (seen >> i) & 1u;
-        p[i] = on ? __builtin_amdgcn_exp2f(y[i] - ref) : 0.f;
-        pv[i] = on ? p[i] * half_lo(t.vm[i >> 2][i & 3]) : 0.f;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w.l[n] += p[i];
-      const float lo = half_hi(t.vm[i >> 2][i & 3]);
-      w.low[n] = __builtin_fmaf(p[i], edge ? ((seen >> i) & 1u ? lo : 0.f) : lo, __builtin_fmaf(8.f, pv[i], w.low[n]));
-    }
-    const u32x4 b = {F16::pack(16.f * pv[0], 16.f * pv[1]), F16::pack(pv[2], pv[3]), F16::pack(16.f * pv[4], 16.f * pv[5]),
-                     F16::pack(pv[6], pv[7])};
-    pb[n] = __builtin_bit_cast(h8_t, b);
-    w.mid[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(0x88888888u), pb[n], w.mid[n], 0, 0, 0);
-  }
+  for (int n = 0; n < NQ; ++n) w.mid[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(0x88888888u), pb[n], w.mid[n], 0, 0, 0);
 #pragma unroll
   for (int st = 0; st < STEPS; ++st)
 #pragma unroll
@@ -205,6 +209,56 @@ __device__ __forceinline__ void attend_tile(const AttendArgs &a, const Tile<STEP
     }
 }
 
+// Tiles from, from + STEP, ... below `to` of a span.  The next tile's words are asked for where this one's are used up (keys
+// behind the first product, pairs behind the weights, values behind the second product); behind the last tile every lane
+// asks for the same 16 bytes.
+template <bool EDGE, int STEP, int STEPS, int NQ>
+__device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &span, int b, int head, int from, int to, int lane,
+                                             Rows<STEPS, NQ> &w) {
+  if (from >= to) return;
+  const CacheView &c = a.c;
+  const int quad = lane >> 4;
+  Tile<STEPS> t;
+  int i = from, tile = span.tile(i);
+  const uint8_t *p = uniform_tile(c, b, head, tile);
+  bool there = p != nullptr;
+  p = there ? p : c.pages;             // some page, not used
+  load_keys(p, lane * 8, t);
+  load_pairs(p, quad * 16, t);
+  load_values(p, lane * 8, t);
+  while (true) {
+    i += STEP;
+    const bool more = i < to;
+    const int next = more ? span.tile(i) : tile;
+    const uint8_t *pn = uniform_tile(c, b, head, next);
+    const bool next_there = pn != nullptr;
+    pn = next_there ? pn : c.pages;
+    const u32 lane8 = more ? lane * 8 : 0, quad16 = more ? quad * 16 : 0;
+    f32x4 s[NQ][2];
+    scores(t, w, s);
+    __builtin_amdgcn_sched_barrier(0);
+    load_keys(pn, lane8, t);
+    h8_t pb[NQ];
+    if (there) {
+      const int at = tile * 32 + 4 * quad;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const int hi = (w.pos[n] < a.max_len ? w.pos[n] : a.max_len - 1) - at;
+        const int lo = a.window == 0 ? -1 : w.pos[n] - a.window - at;
+        pb[n] = weights<EDGE>(s[n], t, hi, lo, a.sinks - at, n, w);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    load_pairs(pn, quad16, t);
+    if (there) products(t, pb, w);
+    __builtin_amdgcn_sched_barrier(0);
+    load_values(pn, lane8, t);
+    if (!more) break;
+    tile = next;
+    there = next_there;
+  }
+}
+
 __device__ __forceinline__ float quads_sum(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
@@ -212,7 +266,7 @@ __device__ __forceinline__ float quads_sum(float v) {
 
 // SHARE: the waves of a workgroup take other rows of the same keys.  Else: other keys of the same rows.
 template <int STEPS, int NQ, bool SHARE>
-__global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : 4) void owq_attend_kernel(AttendArgs a) {
   constexpr int P = 32 * STEPS;
   __shared__ float red[SHARE ? 1 : kWaves][16][P + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -228,8 +282,8 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kerne
   const int p0 = len - n_new;
   const int pa = p0 + first / a.group;
   const int last = (first + 16 * NQ < n_rows ? first + 16 * NQ : n_rows) - 1;
-  const int pb = p0 + last / a.group;
-  const Span span = visible_tiles(a, pa, pb);
+  const int pb_pos = p0 + last / a.group;
+  const Span span = visible_tiles(a, pa, pb_pos);
   int i0 = split * a.tiles_per_split, i1 = i0 + a.tiles_per_split;
   i1 = i1 < span.count ? i1 : span.count;
   if (a.splits > 1 && i0 >= i1 && split > 0) return;                            // the sum over ranges does not look here
@@ -278,29 +332,21 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : 2) void owq_attend_kerne
     w.mid[n] = zero;
   }
 
-  // tiles of this wave: all of the range, or every kWaves-th
+  // Tiles that every row sees whole lie in one run of the span; the few others are masked key by key.
   constexpr int kStep = SHARE ? 1 : kWaves;
-  auto edge = [&](const Tile<STEPS> &t) {
-    const bool all = t.there && t.key0 + 31 <= pa && t.key0 + 31 < a.max_len &&
-                     (a.window == 0 || t.key0 > pb - a.window || t.key0 + 31 < a.sinks);
-    return !all;
-  };
-  int i = i0 + (SHARE ? 0 : wave);
-  if (i < i1) {
-    Tile<STEPS> x, y;
-    load_tile<STEPS>(c, b, head, span.tile(i), lane, x);
-    while (true) {
-      const int j = i + kStep < i1 ? i + kStep : i;
-      load_tile<STEPS>(c, b, head, span.tile(j), lane, y);
-      attend_tile<STEPS, NQ>(a, x, lane, edge(x), w);
-      i += kStep;
-      if (i >= i1) break;
-      const int k = i + kStep < i1 ? i + kStep : i;
-      load_tile<STEPS>(c, b, head, span.tile(k), lane, x);
-      attend_tile<STEPS, NQ>(a, y, lane, edge(y), w);
-      i += kStep;
-      if (i >= i1) break;
-    }
+  int w0 = span.sink_tiles, w1 = span.sink_tiles;
+  {
+    const int low = a.window > 0 && pb_pos >= a.window ? (pb_pos - a.window + 32) / 32 : 0;       // first tile inside every row's window
+    const int end = (pa + 1 < a.max_len ? pa + 1 : a.max_len) / 32;                               // first tile with a key that some row does not see
+    w0 += low > span.low ? low - span.low : 0;
+    w1 += end > span.low ? end - span.low : 0;
+    w1 = w1 < w0 ? w0 : w1;
+  }
+  {
+    const int from = i0 > w0 ? i0 : w0, to = i1 < w1 ? i1 : w1;
+    attend_tiles<false, kStep>(a, span, b, head, from + (SHARE ? 0 : wave), to, lane, w);
+    attend_tiles<true, kStep>(a, span, b, head, i0 + (SHARE ? 0 : wave), i1 < w0 ? i1 : w0, lane, w);
+    attend_tiles<true, kStep>(a, span, b, head, (i0 > w1 ? i0 : w1) + (SHARE ? 0 : wave), i1, lane, w);
   }
 
   // results: column sums of a row lie in the lanes of its column
@@ -420,7 +466,7 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   p.group = a.q_heads / d.kv_heads;
   p.rows = (int)std::min<int64_t>((int64_t)a.max_new * p.group, 0x7fffffff);
   p.share_keys = p.rows > 64;
-  p.col_tiles = p.rows <= 16 ? 1 : p.rows <= 32 ? 2 : 4;
+  p.col_tiles = p.rows <= 16 ? 1 : p.rows <= 32 || p.share_keys ? 2 : 4;
   const int block = 16 * p.col_tiles * (p.share_keys ? kWaves : 1);
   p.row_blocks = (p.rows + block - 1) / block;
   int64_t seen = std::min<int64_t>(a.max_len, (int64_t)d.table_stride * d.page_size);
@@ -444,7 +490,7 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
 
 template <int STEPS>
 static void launch_steps(const AttendArgs &a, const AttendPlan &p, dim3 grid, hipStream_t s) {
-  if (p.share_keys) owq_attend_kernel<STEPS, 4, true><<<grid, 64 * kWaves, 0, s>>>(a);
+  if (p.share_keys) owq_attend_kernel<STEPS, 2, true><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (p.col_tiles == 1) owq_attend_kernel<STEPS, 1, false><<<grid, 64 * kWaves, 0, s>>>(a);
   else if (p.col_tiles == 2) owq_attend_kernel<STEPS, 2, false><<<grid, 64 * kWaves, 0, s>>>(a);
   else owq_attend_kernel<STEPS, 4, false><<<grid, 64 * kWaves, 0, s>>>(a);

@@ -15,6 +15,16 @@ __device__ __forceinline__ uint8_t *cache_tile(const CacheView &c, int b, int he
   return c.pages + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * c.tile_bytes;
 }
 
+// The same for a tile that is the same for all lanes of a wave: the address stays in scalar registers.
+__device__ __forceinline__ const uint8_t *uniform_tile(const CacheView &c, int b, int head, int tile) {
+  const int slot = tile >> c.page_shift;
+  if (slot >= c.table_stride) return nullptr;
+  const int page = __builtin_amdgcn_readfirstlane(c.table[(int64_t)b * c.table_stride + slot]);
+  if (page < 0 || page >= c.n_pages) return nullptr;
+  const int in_page = tile & ((1 << c.page_shift) - 1);
+  return c.pages + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * c.tile_bytes;
+}
+
 // Eight codes in bytes (elements 0..3 in a, 4..7 in b) to their word: element e at nibble e / 2 + 4 (e % 2).
 __device__ __forceinline__ u32 word_of_bytes(u32 a, u32 b) {
   // even elements in the low half, odd ones in the high half

@@ -525,7 +525,7 @@ owq_status_t owq_cache_attention(const owq_cache_desc_t *desc, const owq_attenti
  * temperature 1 where it is 0).  Logits of -infinity are never chosen.  A row whose largest
  * logit is not finite, or that has a NaN in it, or whose temperature is negative or NaN, has no
  * token: -1 and NaN; so has a row whose temperature is not 0 without noise.
- * Probabilities are summed in 40-bit fixed point, so no order of summation shows.
+ * Probabilities are summed as integers, in units of 2^-31 of the largest, so no order of summation shows.
  * n_rows == 0 is a no-op; vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
  * workspace: owq_sample_workspace_bytes bytes, 16-byte aligned (may be NULL if the answer is 0),
  * contents undefined before and after.

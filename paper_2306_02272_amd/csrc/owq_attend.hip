@@ -220,17 +220,20 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &sp
   const int quad = lane >> 4;
   Tile<STEPS> t;
   int i = from, tile = span.tile(i);
-  const uint8_t *p = uniform_tile(c, b, head, tile);
+  const uint8_t *p = tile_in_page(c, page_of_tile(c, b, tile), head, tile);
   bool there = p != nullptr;
   p = there ? p : c.pages;             // some page, not used
   load_keys(p, lane * 8, t);
   load_pairs(p, quad * 16, t);
   load_values(p, lane * 8, t);
+  int next = i + STEP < to ? span.tile(i + STEP) : tile;
+  int next_page = page_of_tile(c, b, next);
   while (true) {
     i += STEP;
     const bool more = i < to;
-    const int next = more ? span.tile(i) : tile;
-    const uint8_t *pn = uniform_tile(c, b, head, next);
+    const uint8_t *pn = tile_in_page(c, next_page, head, next);
+    const int after = i + STEP < to ? span.tile(i + STEP) : next;
+    next_page = page_of_tile(c, b, after);
     const bool next_there = pn != nullptr;
     pn = next_there ? pn : c.pages;
     const u32 lane8 = more ? lane * 8 : 0, quad16 = more ? quad * 16 : 0;
@@ -255,6 +258,7 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &sp
     load_values(pn, lane8, t);
     if (!more) break;
     tile = next;
+    next = after;
     there = next_there;
   }
 }
@@ -477,8 +481,12 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   if (!p.share_keys) {
     // enough workgroups for every compute unit, two tiles per wave at least
     const int64_t base = (int64_t)d.n_seqs * d.kv_heads * p.row_blocks;
-    const int64_t want = std::max<int64_t>(1, 2048 / std::max<int64_t>(1, base));
-    const int most = std::max(1, tiles / (2 * kWaves));
+#ifndef WGS
+#define WGS 2048
+#define TPW 2
+#endif
+    const int64_t want = std::max<int64_t>(1, WGS / std::max<int64_t>(1, base));
+    const int most = std::max(1, tiles / (TPW * kWaves));
     const int splits = (int)std::min<int64_t>(want, most);
     p.tiles_per_split = std::max(1, (tiles + splits - 1) / splits);
     p.splits = std::max(1, (tiles + p.tiles_per_split - 1) / p.tiles_per_split);

@@ -15,14 +15,16 @@ __device__ __forceinline__ uint8_t *cache_tile(const CacheView &c, int b, int he
   return c.pages + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * c.tile_bytes;
 }
 
-// The same for a tile that is the same for all lanes of a wave: the address stays in scalar registers.
-__device__ __forceinline__ const uint8_t *uniform_tile(const CacheView &c, int b, int head, int tile) {
-  const int slot = tile >> c.page_shift;
-  if (slot >= c.table_stride) return nullptr;
-  const int page = __builtin_amdgcn_readfirstlane(c.table[(int64_t)b * c.table_stride + slot]);
-  if (page < 0 || page >= c.n_pages) return nullptr;
+// The same in two steps, for a wave that walks over tiles: the page of a tile within the table (asked for a tile ahead of
+// its use: a scalar load), and its address (scalar arithmetic), nullptr where it is no page.
+__device__ __forceinline__ int page_of_tile(const CacheView &c, int b, int tile) {
+  return c.table[(int64_t)b * c.table_stride + (tile >> c.page_shift)];
+}
+__device__ __forceinline__ const uint8_t *tile_in_page(const CacheView &c, int page, int head, int tile) {
+  page = __builtin_amdgcn_readfirstlane(page);
   const int in_page = tile & ((1 << c.page_shift) - 1);
-  return c.pages + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * c.tile_bytes;
+  const uint8_t *p = c.pages + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * c.tile_bytes;
+  return page >= 0 && page < c.n_pages ? p : nullptr;
 }
 
 // Eight codes in bytes (elements 0..3 in a, 4..7 in b) to their word: element e at nibble e / 2 + 4 (e % 2).

@@ -31,14 +31,14 @@ constexpr float kLog2e = 1.44269504089f, kLn2 = 0.69314718056f;
 struct SampleShared {
   u64 mass[kMassBins];
   u32 count[kBins];
-  u32 list_key[kList], list_at[kList], sure_key[kList], sure_at[kList];
+  u64 list[kList], sure[kList];   // key << 32 | ~index: larger comes first
   u32 n_list, n_sure;
   u64 wave_mass[16];
   u32 wave_count[16];
   u64 best[16];
   float sum[16];
   u32 digit;
-  u32 cut_key, cut_at;
+  u64 cut;
   u64 total;
 };
 
@@ -58,51 +58,54 @@ __device__ __forceinline__ float logit_at(const void *row, int i) {
   return TYPE == OWQ_TYPE_F16 ? F16::lo(w) : BF16::lo(w);
 }
 
+// A value from another lane of the wave, `none` where there is no such lane: the six steps of a scan over 64 lanes
+// (1, 2, 4 and 8 lanes down within rows of 16, then the last lane of a row to the next row, and of the lower half to the upper).
+template <int STEP>
+__device__ __forceinline__ u32 from_lane(u32 v, u32 none) {
+  constexpr int ctrl = STEP == 0 ? 0x111 : STEP == 1 ? 0x112 : STEP == 2 ? 0x114 : STEP == 3 ? 0x118 : STEP == 4 ? 0x142 : 0x143;
+  constexpr int rows = STEP == 4 ? 0xa : STEP == 5 ? 0xc : 0xf;
+  return (u32)__builtin_amdgcn_update_dpp((int)none, (int)v, ctrl, rows, 0xf, false);
+}
+template <int STEP>
+__device__ __forceinline__ u64 from_lane(u64 v, u64 none) {
+  return (u64)from_lane<STEP>((u32)(v >> 32), (u32)(none >> 32)) << 32 | from_lane<STEP>((u32)v, (u32)none);
+}
+template <int STEP>
+__device__ __forceinline__ float from_lane(float v, float none) {
+  return __builtin_bit_cast(float, from_lane<STEP>(__builtin_bit_cast(u32, v), __builtin_bit_cast(u32, none)));
+}
+// Inclusive scan over the wave's lanes; the last lane holds the result over all of them.
+template <class T, class F>
+__device__ __forceinline__ T wave_scan(T v, T none, F &&f) {
+  v = f(v, from_lane<0>(v, none));
+  v = f(v, from_lane<1>(v, none));
+  v = f(v, from_lane<2>(v, none));
+  v = f(v, from_lane<3>(v, none));
+  v = f(v, from_lane<4>(v, none));
+  return f(v, from_lane<5>(v, none));
+}
+template <class T, class F>
+__device__ __forceinline__ T block_reduce(T v, T none, T *part, F &&f) {
+  v = wave_scan(v, none, f);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int i = 1; i < kSampleThreads / 64; ++i) v = f(v, part[i]);
+  return v;
+}
 __device__ __forceinline__ u64 block_max(u64 v, SampleShared &sh) {
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const u64 o = __shfl_xor(v, s);
-    v = o > v ? o : v;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sh.best[0];
-  for (int i = 1; i < kSampleThreads / 64; ++i) v = sh.best[i] > v ? sh.best[i] : v;
-  return v;
+  return block_reduce(v, (u64)0, sh.best, [](u64 a, u64 b) { return a > b ? a : b; });
 }
-
 __device__ __forceinline__ u64 block_add(u64 v, SampleShared &sh) {
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) v += __shfl_xor(v, s);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0;
-  for (int i = 0; i < kSampleThreads / 64; ++i) v += sh.best[i];
-  return v;
+  return block_reduce(v, (u64)0, sh.best, [](u64 a, u64 b) { return a + b; });
 }
-
 __device__ __forceinline__ float block_top(float v, SampleShared &sh) {
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) v = fmaxf(v, __shfl_xor(v, s));
-  if ((threadIdx.x & 63) == 0) sh.sum[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sh.sum[0];
-  for (int i = 1; i < kSampleThreads / 64; ++i) v = fmaxf(v, sh.sum[i]);
-  __syncthreads();
-  return v;
+  return block_reduce(v, -__builtin_inff(), sh.sum, [](float a, float b) { return fmaxf(a, b); });
 }
-
 __device__ __forceinline__ float block_sum(float v, SampleShared &sh) {
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) v += __shfl_xor(v, s);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.sum[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int i = 0; i < kSampleThreads / 64; ++i) v += sh.sum[i];
-  return v;
+  return block_reduce(v, 0.f, sh.sum, [](float a, float b) { return a + b; });
 }
 
 __device__ __forceinline__ u32 mass_of(float x, float top, float rate) {
@@ -139,15 +142,8 @@ __device__ u32 select_key(const void *row, int vocab, float top, float rate, u32
       u32 n = sh.count[d];
       const u64 m0 = m;
       const u32 n0 = n;
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) {
-        const u64 mo = __shfl_up(m, s);
-        const u32 no = __shfl_up(n, s);
-        if (lane >= s) {
-          m += mo;
-          n += no;
-        }
-      }
+      m = wave_scan(m, (u64)0, [](u64 a, u64 b) { return a + b; });
+      n = wave_scan(n, 0u, [](u32 a, u32 b) { return a + b; });
       if (lane == 63) {
         sh.wave_mass[threadIdx.x >> 6] = m;
         sh.wave_count[threadIdx.x >> 6] = n;
@@ -251,12 +247,7 @@ __device__ Cut general_cut(const void *row, int vocab, int k, float p, float top
 // Threads' counts to their first places; *all = the sum.
 __device__ __forceinline__ u32 block_places(u32 n, u32 *all, SampleShared &sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u32 sum = n;
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const u32 o = __shfl_up(sum, s);
-    sum += lane >= s ? o : 0u;
-  }
+  const u32 sum = wave_scan(n, 0u, [](u32 a, u32 b) { return a + b; });
   __syncthreads();
   if (lane == 63) sh.wave_count[wave] = sum;
   __syncthreads();
@@ -297,26 +288,33 @@ struct RowView {
   template <class G>
   __device__ __forceinline__ void batches(G &&g) const {
     const u32 low = TYPE == OWQ_TYPE_F32 ? 0xff800000u : TYPE == OWQ_TYPE_F16 ? 0xfc00fc00u : 0xff80ff80u;   // -infinity past the end
-    for (int base = 0; base < n_units; base += kSampleThreads * kUnroll) {
-      u32x4 v[kUnroll];
-#pragma unroll
-      for (int j = 0; j < kUnroll; ++j) v[j] = units[min(base + j * kSampleThreads + (int)threadIdx.x, n_units - 1)];
+    // the logits beside the units come last, one per thread: one copy of g's code, not two
+    for (int base = 0;; base += kSampleThreads * kUnroll) {
+      const bool in_units = base < n_units;
       float x[16];
+      if (in_units) {
+        u32x4 v[kUnroll];
 #pragma unroll
-      for (int j = 0; j < kUnroll; ++j) {
-        const bool on = base + j * kSampleThreads + (int)threadIdx.x < n_units;
-        v[j] = on ? v[j] : (u32x4){low, low, low, low};
+        for (int j = 0; j < kUnroll; ++j) v[j] = units[min(base + j * kSampleThreads + (int)threadIdx.x, n_units - 1)];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) x[j * kPer + e] = get(v[j], e);
+        for (int j = 0; j < kUnroll; ++j) {
+          const bool on = base + j * kSampleThreads + (int)threadIdx.x < n_units;
+          v[j] = on ? v[j] : (u32x4){low, low, low, low};
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) x[j * kPer + e] = get(v[j], e);
+        }
+      } else {
+        if (n_rest == 0) break;
+#pragma unroll
+        for (int i = 1; i < 16; ++i) x[i] = -__builtin_inff();
+        x[0] = (int)threadIdx.x < n_rest ? logit_at<TYPE>(row, rest(threadIdx.x)) : -__builtin_inff();
       }
-      g(x, [&](int i) { return first + (base + (i / kPer) * kSampleThreads + (int)threadIdx.x) * kPer + i % kPer; });
+      g(x, [&](int i) {
+        return in_units ? first + (base + (i / kPer) * kSampleThreads + (int)threadIdx.x) * kPer + i % kPer
+                        : (int)threadIdx.x < n_rest ? rest(threadIdx.x) : 0;
+      });
+      if (!in_units) break;
     }
-    float x[16];
-    const bool on = (int)threadIdx.x < n_rest;
-    x[0] = on ? logit_at<TYPE>(row, rest(threadIdx.x)) : -__builtin_inff();
-#pragma unroll
-    for (int i = 1; i < 16; ++i) x[i] = -__builtin_inff();
-    g(x, [&](int) { return on ? rest(threadIdx.x) : 0; });
   }
   template <class F>
   __device__ __forceinline__ void each(F &&f) const {
@@ -327,47 +325,49 @@ struct RowView {
   }
 };
 
+__device__ __forceinline__ u64 entry_of(float v, u32 at) { return (u64)key_of(v) << 32 | (0xffffffffu - at); }
+__device__ __forceinline__ float entry_logit(u64 e) { return logit_of((u32)(e >> 32)); }
+__device__ __forceinline__ u32 entry_at(u64 e) { return 0xffffffffu - (u32)e; }
+
 // A list of logits in LDS, in no order.
 struct List {
-  u32 *key, *at, *n;
-  // the logits of `bits` behind the entries that are there; entries past kList are counted only
-  template <class I>
-  __device__ __forceinline__ void add(const float (&x)[16], u32 bits, I &&index) {
+  u64 *entry;
+  u32 *n;
+  // the logits of `bits` behind the entries that are there, read again as they are few; entries past kList are counted only
+  template <int TYPE, class I>
+  __device__ __forceinline__ void add(const RowView<TYPE> &x, u32 bits, I &&index) {
     if (!__any(bits != 0)) return;
     const int lane = threadIdx.x & 63;
     const u32 mine = (u32)__popc(bits);
-    u32 sum = mine;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const u32 o = __shfl_up(sum, s);
-      sum += lane >= s ? o : 0u;
-    }
+    const u32 sum = wave_scan(mine, 0u, [](u32 a, u32 b) { return a + b; });
     u32 base = 0;
     if (lane == 63) base = atomicAdd(n, sum);
-    u32 place = __shfl(base, 63) + sum - mine;
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if ((bits >> i) & 1u) {
-        if (place < (u32)kList) {
-          key[place] = key_of(x[i]);
-          at[place] = (u32)index(i);
-        }
-        ++place;
-      }
+    u32 place = (u32)__builtin_amdgcn_readlane((int)base, 63) + sum - mine;
+    for (; bits != 0 && place < (u32)kList; bits &= bits - 1, ++place) {
+      const int i = index(__ffs(bits) - 1);
+      entry[place] = entry_of(logit_at<TYPE>(x.row, i), (u32)i);
+    }
   }
 };
 
 // What precedes a logit in a list of n: how many, and their mass.
-__device__ __forceinline__ void precede(const u32 *list_key, const u32 *list_at, const u32 *list_mass, u32 n, u32 key, u32 at, u32 *rank,
-                                        u64 *mass) {
+__device__ __forceinline__ void precede(const u64 *list, const u32 *list_mass, u32 n, u64 me, u32 *rank, u64 *mass) {
   u32 c = 0;
   u64 m = 0;
-#pragma unroll 4
-  for (u32 j = 0; j < n; ++j) {
-    const u32 kk = list_key[j];
-    const bool before = kk > key || (kk == key && list_at[j] < at);
-    c += before ? 1u : 0u;
-    m += before ? list_mass[j] : 0u;
+  for (u32 j = 0; j < n; j += 8) {
+    u64 e[8];
+    u32 w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e[i] = list[j + i];           // past n: entries of 0, before nothing
+      w[i] = list_mass[j + i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool before = e[i] > me;
+      c += before ? 1u : 0u;
+      m += before ? w[i] : 0u;
+    }
   }
   *rank = c;
   *mass = m;
@@ -391,6 +391,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   const bool by_k = t > 0.f && k >= 1 && k < a.vocab, short_k = by_k && k <= kList / 2, by_p = t > 0.f && !by_k && p < 1.f;
   const float least = mp > 0.f ? top + __builtin_amdgcn_logf(mp) / rate : bottom;     // z >= max z + ln min_p, on logits
   if (threadIdx.x == 0) sh.n_sure = sh.n_list = 0;
+  sh.list[threadIdx.x] = 0;
 
   // what the second pass needs: the least candidate for top-k, empty bins for top-p
   float lo = __builtin_inff();
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   }
   __syncthreads();
 
-  List list = {sh.list_key, sh.list_at, &sh.n_list}, sure = {sh.sure_key, sh.sure_at, &sh.n_sure};
+  List list = {sh.list, &sh.n_list}, sure = {sh.sure, &sh.n_sure};
   float total = 0.f;
   u64 m = 0;
   x.batches([&](const float (&v)[16], auto &&index) {
@@ -432,7 +433,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
         m += w;
       }
     }
-    if (short_k) list.add(v, bits, index);
+    if (short_k) list.add(x, bits, index);
   });
   total = block_sum(total, sh);           // NaN if a logit is (or the top infinite)
   if (!(__builtin_fabsf(top) < __builtin_inff()) || total != total || !(t >= 0.f) || (t > 0.f && a.noise == nullptr)) {
@@ -444,8 +445,8 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   }
 
   const float *noise = a.noise + (int64_t)r * a.noise_row;
-  auto score = [&](float v, u32 at) {
-    return (u64)key_of(__builtin_fmaf(v, rate, -__builtin_amdgcn_logf(noise[at]))) << 32 | (0xffffffffu - at);
+  auto score = [&](u64 e) {
+    return entry_of(__builtin_fmaf(entry_logit(e), rate, -__builtin_amdgcn_logf(noise[entry_at(e)])), entry_at(e));
   };
   u64 best = 0;
   Cut cut = {key_of(bottom) + 1u, 0xffffffffu};
@@ -465,20 +466,20 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   } else if (short_k && sh.n_list <= (u32)kList) {
     const u32 n = sh.n_list;
     const bool on = threadIdx.x < n;
-    const u32 key = on ? sh.list_key[threadIdx.x] : 0u, at = on ? sh.list_at[threadIdx.x] : 0u;
-    const float v = logit_of(key);
+    const u64 me = sh.list[threadIdx.x];
+    const float v = entry_logit(me);
     const u32 w = on ? mass_of(v, top, rate) : 0u;
     sh.count[threadIdx.x] = w;
     __syncthreads();
     u32 rank;
     u64 ahead;
-    precede(sh.list_key, sh.list_at, sh.count, on ? n : 0u, key, at, &rank, &ahead);
+    precede(sh.list, sh.count, on ? n : 0u, me, &rank, &ahead);
     bool stays = on && rank < (u32)k;
     if (p < 1.f) {
       const u64 mass = block_add(stays ? (u64)w : 0ull, sh);
       stays = stays && (double)ahead < fmax((double)p * (double)mass, 1.0);
     }
-    if (stays && (v >= least || v == top)) best = score(v, at);
+    if (stays && (v >= least || v == top)) best = score(me);
     done = true;
   } else if (by_k) {
     cut = general_cut<TYPE>(row, a.vocab, k, p, top, rate, sh);
@@ -492,11 +493,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     for (int j = 0; j < kEach; ++j) sum += own[j] = sh.mass[threadIdx.x * kEach + j];
     const u64 mine_all = sum;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const u64 o = __shfl_up(sum, s);
-      sum += lane >= s ? o : 0ull;
-    }
+    sum = wave_scan(sum, (u64)0, [](u64 a, u64 b) { return a + b; });
     if (lane == 63) sh.wave_mass[wave] = sum;
     __syncthreads();
     u64 ahead = sum - mine_all;
@@ -522,8 +519,8 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
         inside |= on && b == bin ? 1u << i : 0u;
         before |= on && b < bin ? 1u << i : 0u;
       }
-      list.add(v, inside, index);
-      sure.add(v, before, index);
+      list.add(x, inside, index);
+      sure.add(x, before, index);
     });
     __syncthreads();
     const u32 n = sh.n_list, n_sure = sh.n_sure;
@@ -531,31 +528,28 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       cut = general_cut<TYPE>(row, a.vocab, 0, p, top, rate, sh);
     } else {
       const bool on = threadIdx.x < n;
-      const u32 key = on ? sh.list_key[threadIdx.x] : 0u, at = on ? sh.list_at[threadIdx.x] : 0u;
-      sh.count[threadIdx.x] = on ? mass_of(logit_of(key), top, rate) : 0u;
+      const u64 me = sh.list[threadIdx.x];
+      sh.count[threadIdx.x] = on ? mass_of(entry_logit(me), top, rate) : 0u;
       __syncthreads();
       u32 rank;
       u64 mass;
-      precede(sh.list_key, sh.list_at, sh.count, on ? n : 0u, key, at, &rank, &mass);
+      precede(sh.list, sh.count, on ? n : 0u, me, &rank, &mass);
       const bool stays = on && (double)(above + mass) < want;
       if (n_sure <= (u32)kList) {
-        if (stays) best = score(logit_of(key), at);
+        if (stays) best = score(me);
         if (threadIdx.x < n_sure) {
-          const u64 o = score(logit_of(sh.sure_key[threadIdx.x]), sh.sure_at[threadIdx.x]);
+          const u64 o = score(sh.sure[threadIdx.x]);
           best = o > best ? o : best;
         }
         done = true;
       } else {
         // the last that stays is the cut (above all of the bin if none does)
         const u64 last = block_max(stays ? (u64)rank + 1 : 0ull, sh);
-        if (threadIdx.x == 0) sh.cut_key = 0xffffffffu;
+        if (threadIdx.x == 0) sh.cut = ~0ull;
         __syncthreads();
-        if (stays && (u64)rank + 1 == last) {
-          sh.cut_key = key;
-          sh.cut_at = at;
-        }
+        if (stays && (u64)rank + 1 == last) sh.cut = me;
         __syncthreads();
-        cut = Cut{sh.cut_key, sh.cut_at};
+        cut = Cut{(u32)(sh.cut >> 32), entry_at(sh.cut)};
       }
     }
   }
@@ -577,7 +571,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       for (int i = 0; i < 16; ++i) u[i] = noise[min(index(i), a.vocab - 1)];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const u64 o = (u64)key_of(__builtin_fmaf(v[i], rate, -__builtin_amdgcn_logf(u[i]))) << 32 | (0xffffffffu - (u32)index(i));
+        const u64 o = entry_of(__builtin_fmaf(v[i], rate, -__builtin_amdgcn_logf(u[i])), (u32)index(i));
         best = ((bits >> i) & 1u) && o > best ? o : best;
       }
     });

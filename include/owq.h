@@ -527,14 +527,10 @@ owq_status_t owq_cache_attention(const owq_cache_desc_t *desc, const owq_attenti
  * token: -1 and NaN; so has a row whose temperature is not 0 without noise.
  * Probabilities are summed as integers, in units of 2^-31 of the largest, so no order of summation shows.
  * n_rows == 0 is a no-op; vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
- * workspace: owq_sample_workspace_bytes bytes, 16-byte aligned (may be NULL if the answer is 0),
- * contents undefined before and after.
  */
-owq_status_t owq_sample_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t type, size_t *bytes);
 owq_status_t owq_sample(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row,
                         const float *noise, int64_t noise_row, const float *temperature, const int32_t *top_k,
-                        const float *top_p, const float *min_p, int32_t *token, float *logprob, void *workspace,
-                        size_t workspace_bytes, void *stream);
+                        const float *top_p, const float *min_p, int32_t *token, float *logprob, void *stream);
 
 const char *owq_status_str(owq_status_t s);
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -33,7 +34,7 @@ EXPORTS = ["owq_geometry", "owq_packed_bytes", "owq_pack_host", "owq_unpack_code
            "owq_backward_workspace_bytes", "owq_linear_backward", "owq_probe_read", "owq_probe_read_write", "owq_probe_empty", "owq_probe_alu", "owq_probe_mfma", "owq_workspace_bytes", "owq_linear_ws", "owq_linear_static",
            "owq_qk_norm_rope", "owq_qk_norm_rope_backward_workspace_bytes", "owq_qk_norm_rope_backward", "owq_cache_page_bytes",
            "owq_cache_append", "owq_cache_read", "owq_cache_attention_workspace_bytes", "owq_cache_attention",
-           "owq_sample_workspace_bytes", "owq_sample", "owq_status_str"]
+           "owq_sample", "owq_status_str"]
 
 
 class OwqError(RuntimeError):
@@ -133,10 +134,9 @@ def lib():
         L.owq_cache_page_bytes.argtypes = [P, C.POINTER(SZ)]
         L.owq_cache_append.argtypes = [P] * 7 + [I32] * 3 + [I64] * 4 + [P]
         L.owq_cache_read.argtypes = [P] * 6 + [I32] * 3 + [P]
-        L.owq_cache_attention_workspace_bytes.argtypes = [P, P, C.POINTER(SZ)]
+        L.owq_cache_attention_workspace_bytes.argtypes = [P, P, C.POINTER(SZ)]   # takes a c_size_t as it is
         L.owq_cache_attention.argtypes = [P] * 10 + [SZ, P]
-        L.owq_sample_workspace_bytes.argtypes = [I32, I32, I32, C.POINTER(SZ)]
-        L.owq_sample.argtypes = [P, I32, I32, I32, I64, P, I64] + [P] * 7 + [SZ, P]
+        L.owq_sample.argtypes = [P, I32, I32, I32, I64, P, I64] + [P] * 7
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.owq_status_str.argtypes = [C.c_int]
@@ -420,139 +420,156 @@ def owq_cache_attention(desc: CacheDesc, att: AttentionDesc, q_ptr, pages_ptr, t
                                      lse_ptr, workspace_ptr, workspace_bytes, stream), "owq_cache_attention")
 
 
-def owq_sample_workspace_bytes(n_rows: int, vocab: int, type: int) -> int:
-    n = C.c_size_t(0)
-    _check(lib().owq_sample_workspace_bytes(n_rows, vocab, type, C.byref(n)), "owq_sample_workspace_bytes")
-    return int(n.value)
-
-
 def owq_sample(logits_ptr, type: int, n_rows: int, vocab: int, logits_row: int, noise_ptr, noise_row: int, temperature_ptr, top_k_ptr,
-               top_p_ptr, min_p_ptr, token_ptr, logprob_ptr, workspace_ptr, workspace_bytes: int, stream: int = 0) -> None:
+               top_p_ptr, min_p_ptr, token_ptr, logprob_ptr, stream: int = 0) -> None:
     _check(lib().owq_sample(logits_ptr, type, n_rows, vocab, logits_row, noise_ptr, noise_row, temperature_ptr, top_k_ptr, top_p_ptr,
-                            min_p_ptr, token_ptr, logprob_ptr, workspace_ptr, workspace_bytes, stream), "owq_sample")
+                            min_p_ptr, token_ptr, logprob_ptr, stream), "owq_sample")
 
 
-_TYPES = None
+_TORCH = None
+_TYPES = {}
+# the layouts of owq_rope_desc_t, owq_cache_desc_t and owq_attention_desc_t: packed bytes take a fifth of a Structure's time
+_ROPE = struct.Struct("@8ifi8q")
+_CACHE = struct.Struct("@6i")
+_ATTENTION = struct.Struct("@7if2q")
 
 
-def _type_of(t, f32=False):
-    """OWQ_TYPE_* of a tensor's type."""
-    global _TYPES
-    if _TYPES is None:
+def _torch():
+    global _TORCH
+    if _TORCH is None:
         import torch
-        _TYPES = {torch.float16: OWQ_TYPE_F16, torch.bfloat16: OWQ_TYPE_BF16, torch.float32: OWQ_TYPE_F32}
-    n = _TYPES.get(t.dtype, -1)
-    assert n >= 0 and (f32 or n != OWQ_TYPE_F32), t.dtype
+        _TYPES.update({torch.float16: OWQ_TYPE_F16, torch.bfloat16: OWQ_TYPE_BF16, torch.float32: OWQ_TYPE_F32})
+        _TORCH = torch
+    return _TORCH
+
+
+def _type_of(t, most=OWQ_TYPE_BF16):
+    """OWQ_TYPE_* of a tensor's type."""
+    n = _TYPES.get(t.dtype, 99)
+    assert n <= most, t.dtype
     return n
 
 
-def _heads(x, what):
-    """[rows, heads, head size] on the GPU, last axis contiguous."""
-    assert x.dim() == 3 and x.is_cuda and (x.stride(2) == 1 or x.shape[2] == 1), (what, x.shape, x.stride())
-    return x
+def _ptr_of(x):
+    return 0 if x is None else x.data_ptr()
 
 
 def _int32(x, n, what):
-    assert x.is_cuda and x.is_contiguous() and x.numel() >= n and "int32" in str(x.dtype), (what, x.dtype, x.shape)
+    assert x.is_cuda and x.dtype is _TORCH.int32 and x.is_contiguous() and x.numel() >= n, (what, x.dtype, x.shape)
     return x.data_ptr()
 
 
-def _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved):
-    import torch
-    _heads(q, "q"), _heads(k, "k")
+def _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq=None, dk=None):
+    """(description, tokens) after the checks that need the tensors; the library checks the rest."""
+    torch = _torch()
     tokens, q_heads, dim = q.shape
-    assert k.shape[0] == tokens and k.shape[2] == dim and k.dtype == q.dtype and k.device == q.device, (q.shape, k.shape)
-    assert cos.dtype == torch.float32 and sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape
-    assert cos.is_cuda and sin.is_cuda and cos.is_contiguous() and sin.is_contiguous()
+    k_tokens, kv_heads, k_dim = k.shape
+    (qt, qh, q1), (kt, kh, k1) = q.stride(), k.stride()
+    n_positions, half = cos.shape
+    f32 = torch.float32
+    assert q.is_cuda and k.is_cuda and k_tokens == tokens and k_dim == dim and k.dtype is q.dtype and q1 == 1 and k1 == 1, (q.shape, k.shape)
+    assert cos.dtype is f32 and sin.dtype is f32 and cos.is_cuda and sin.is_cuda and cos.is_contiguous() and sin.is_contiguous()
+    assert cos.shape == sin.shape
     for w in (wq, wk):
-        assert w is None or (w.dtype == q.dtype and w.is_cuda and w.is_contiguous() and w.numel() == dim)
-    _int32(positions, tokens, "positions")
-    return RopeDesc(tokens, q_heads, k.shape[1], dim, 2 * cos.shape[1], int(interleaved), _type_of(q), cos.shape[0], eps, 0,
-                    q.stride(0), q.stride(1), k.stride(0), k.stride(1), 0, 0, 0, 0)
+        assert w is None or (w.dtype is q.dtype and w.is_cuda and w.is_contiguous() and w.numel() == dim)
+    dqt = dqh = dkt = dkh = 0
+    if dq is not None:
+        for d, x in ((dq, q), (dk, k)):
+            assert d.is_cuda and d.shape == x.shape and d.dtype is x.dtype and d.stride(2) == 1
+        dqt, dqh, dkt, dkh = dq.stride(0), dq.stride(1), dk.stride(0), dk.stride(1)
+    return _ROPE.pack(tokens, q_heads, kv_heads, dim, 2 * half, interleaved, _type_of(q), n_positions, eps, 0, qt, qh, kt, kh, dqt, dqh, dkt,
+                      dkh), tokens
 
 
 def qk_norm_rope(q, k, cos, sin, positions, wq=None, wk=None, eps=1e-6, interleaved=False, out=None):
     """owq_qk_norm_rope on CUDA tensors: q [tokens, query heads, head size] and k [tokens, key heads, head size], fp16 or bf16, as
     slices of one tensor if need be; cos, sin fp32 [positions, rotated columns / 2]; positions int32 [tokens]; wq, wk the norms'
     weights or None.  Returns (q, k) turned, packed; `out` = a pair of packed tensors to write to (the inputs' own if packed)."""
-    import torch
-    desc = _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved)
+    desc, tokens = _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved)
     if out is None:
-        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        empty, dtype, device = _TORCH.empty, q.dtype, q.device
+        q_out, k_out = empty(q.shape, dtype=dtype, device=device), empty(k.shape, dtype=dtype, device=device)
     else:
         q_out, k_out = out
         for o, x in ((q_out, q), (k_out, k)):
-            assert o.shape == x.shape and o.dtype == x.dtype and o.is_cuda and o.is_contiguous()
-    owq_qk_norm_rope(desc, q.data_ptr(), k.data_ptr(), 0 if wq is None else wq.data_ptr(), 0 if wk is None else wk.data_ptr(), cos.data_ptr(),
-                     sin.data_ptr(), positions.data_ptr(), q_out.data_ptr(), k_out.data_ptr(), _current_stream(torch))
+            assert o.shape == x.shape and o.dtype is x.dtype and o.is_cuda and o.is_contiguous()
+    status = lib().owq_qk_norm_rope(desc, q.data_ptr(), k.data_ptr(), _ptr_of(wq), _ptr_of(wk), cos.data_ptr(), sin.data_ptr(),
+                                    _int32(positions, tokens, "positions"), q_out.data_ptr(), k_out.data_ptr(), _current_stream(_TORCH))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_qk_norm_rope")
     return q_out, k_out
 
 
 def qk_norm_rope_backward(dq_out, dk_out, q, k, cos, sin, positions, wq=None, wk=None, eps=1e-6, interleaved=False, workspace=None):
     """owq_qk_norm_rope_backward: gradients of qk_norm_rope's outputs to those of q, k and, fp32, of the weights (None without one).
     q, k: the forward's inputs (read only where there is a weight).  Returns (dq, dk, dwq, dwk)."""
-    import torch
-    desc = _rope_desc(q, k, cos, sin, positions, wq, wk, eps, interleaved)
-    for d, x in ((dq_out, q), (dk_out, k)):
-        assert _heads(d, "gradient").shape == x.shape and d.dtype == x.dtype
-    desc.dq_token, desc.dq_head, desc.dk_token, desc.dk_head = dq_out.stride(0), dq_out.stride(1), dk_out.stride(0), dk_out.stride(1)
-    dev = q.device
-    dq, dk = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
-    dwq = None if wq is None else torch.empty(q.shape[2], dtype=torch.float32, device=dev)
-    dwk = None if wk is None else torch.empty(q.shape[2], dtype=torch.float32, device=dev)
-    if workspace is None and (dwq is not None or dwk is not None):
-        workspace = torch.empty(max(16, owq_qk_norm_rope_backward_workspace_bytes(desc)), dtype=torch.uint8, device=dev)
-    owq_qk_norm_rope_backward(desc, dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), 0 if wq is None else wq.data_ptr(),
-                              0 if wk is None else wk.data_ptr(), cos.data_ptr(), sin.data_ptr(), positions.data_ptr(), dq.data_ptr(),
-                              dk.data_ptr(), 0 if dwq is None else dwq.data_ptr(), 0 if dwk is None else dwk.data_ptr(),
-                              0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
-                              _current_stream(torch))
+    desc, tokens = _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq_out, dk_out)
+    empty, dtype, device, dim = _TORCH.empty, q.dtype, q.device, q.shape[2]
+    dq, dk = empty(q.shape, dtype=dtype, device=device), empty(k.shape, dtype=dtype, device=device)
+    dwq = None if wq is None else empty(dim, dtype=_TORCH.float32, device=device)
+    dwk = None if wk is None else empty(dim, dtype=_TORCH.float32, device=device)
+    n = 0
+    if wq is not None or wk is not None:
+        if workspace is None:
+            need = C.c_size_t(0)
+            _check(lib().owq_qk_norm_rope_backward_workspace_bytes(desc, C.byref(need)), "owq_qk_norm_rope_backward_workspace_bytes")
+            workspace = empty(need.value, dtype=_TORCH.uint8, device=device)
+        n = workspace.numel()
+    status = lib().owq_qk_norm_rope_backward(desc, dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), _ptr_of(wq), _ptr_of(wk),
+                                             cos.data_ptr(), sin.data_ptr(), _int32(positions, tokens, "positions"), dq.data_ptr(),
+                                             dk.data_ptr(), _ptr_of(dwq), _ptr_of(dwk), _ptr_of(workspace), n, _current_stream(_TORCH))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_qk_norm_rope_backward")
     return dq, dk, dwq, dwk
 
 
 def cache_empty(n_pages, page_size, kv_heads, head_dim, device="cuda"):
     """Pages for the 4-bit cache: uint8 [n_pages, kv_heads, page_size / 32, bytes of a tile], contents undefined."""
-    import torch
     n = owq_cache_page_bytes(CacheDesc(1, page_size, kv_heads, head_dim, 0, 0))
     tiles = page_size // 32
-    return torch.empty((n_pages, kv_heads, tiles, n // (kv_heads * tiles)), dtype=torch.uint8, device=device)
+    return _torch().empty((n_pages, kv_heads, tiles, n // (kv_heads * tiles)), dtype=_TORCH.uint8, device=device)
 
 
-def _cache_desc(pages, table, n_seqs, kv_heads, dim):
-    assert pages.dim() == 4 and pages.is_cuda and pages.is_contiguous() and pages.element_size() == 1, pages.shape
-    assert table.dim() == 2 and table.shape[0] >= n_seqs
-    _int32(table, 1, "page_table")
+def _cache_args(pages, table, n_seqs, kv_heads, dim):
+    """(description, tokens that a sequence's pages can hold)."""
     n_pages, heads, tiles, size = pages.shape
+    rows, stride = table.shape
+    assert pages.is_cuda and pages.is_contiguous() and pages.dtype is _TORCH.uint8 and table.is_contiguous() and rows >= n_seqs, (pages.shape, table.shape)
     assert heads == kv_heads and size == 32 * ((dim + 31) // 32 * 32) + 256, (pages.shape, kv_heads, dim)
-    return CacheDesc(n_pages, 32 * tiles, heads, dim, n_seqs, table.shape[1])
+    return _CACHE.pack(n_pages, 32 * tiles, heads, dim, n_seqs, stride), 32 * tiles * stride
 
 
 def cache_append(pages, page_table, starts, lengths, k, v, max_new=None):
     """owq_cache_append: rows of k and v [rows, key/value heads, head size] into the pages.  page_table int32 [sequences, pages];
     starts int32 [sequences + 1], the rows of each sequence; lengths int32 [sequences], its tokens with the new ones.
     max_new: the most rows of a sequence (default: all rows; a smaller bound spares empty workgroups)."""
-    import torch
-    _heads(k, "k"), _heads(v, "v")
-    assert k.shape == v.shape and k.dtype == v.dtype
-    n_seqs = lengths.numel()
+    torch = _torch()
     rows, heads, dim = k.shape
-    desc = _cache_desc(pages, page_table, n_seqs, heads, dim)
-    owq_cache_append(desc, pages.data_ptr(), page_table.data_ptr(), _int32(starts, n_seqs + 1, "starts"), _int32(lengths, n_seqs, "lengths"),
-                     k.data_ptr(), v.data_ptr(), _type_of(k), rows, rows if max_new is None else max_new, k.stride(0), k.stride(1),
-                     v.stride(0), v.stride(1), _current_stream(torch))
+    (kr, kh, k1), (vr, vh, v1) = k.stride(), v.stride()
+    assert k.is_cuda and v.is_cuda and v.shape == k.shape and v.dtype is k.dtype and k1 == 1 and v1 == 1, (k.shape, v.shape)
+    n_seqs = lengths.numel()
+    desc, _ = _cache_args(pages, page_table, n_seqs, heads, dim)
+    status = lib().owq_cache_append(desc, pages.data_ptr(), _int32(page_table, n_seqs, "page_table"), _int32(starts, n_seqs + 1, "starts"),
+                                    _int32(lengths, n_seqs, "lengths"), k.data_ptr(), v.data_ptr(), _type_of(k), rows,
+                                    rows if max_new is None else max_new, kr, kh, vr, vh, _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_cache_append")
 
 
 def cache_read(pages, page_table, starts, n_rows, head_dim, max_len=None, dtype=None):
     """owq_cache_read: tokens 0 .. starts[b + 1] - starts[b] - 1 of every sequence as (k, v) [n_rows, key/value heads, head_dim]."""
-    import torch
+    torch = _torch()
     n_seqs = starts.numel() - 1
-    desc = _cache_desc(pages, page_table, n_seqs, pages.shape[1], head_dim)
-    _int32(starts, n_seqs + 1, "starts")
-    shape = (n_rows, pages.shape[1], head_dim)
+    heads, device = pages.shape[1], pages.device
+    desc, _ = _cache_args(pages, page_table, n_seqs, heads, head_dim)
     dtype = torch.float16 if dtype is None else dtype
-    k, v = torch.empty(shape, dtype=dtype, device=pages.device), torch.empty(shape, dtype=dtype, device=pages.device)
-    owq_cache_read(desc, pages.data_ptr(), page_table.data_ptr(), starts.data_ptr(), k.data_ptr(), v.data_ptr(), _type_of(k), n_rows,
-                   n_rows if max_len is None else max_len, _current_stream(torch))
+    shape = (n_rows, heads, head_dim)
+    k, v = torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
+    status = lib().owq_cache_read(desc, pages.data_ptr(), _int32(page_table, n_seqs, "page_table"), _int32(starts, n_seqs + 1, "starts"),
+                                  k.data_ptr(), v.data_ptr(), _type_of(k), n_rows, n_rows if max_len is None else max_len,
+                                  _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_cache_read")
     return k, v
 
 
@@ -561,49 +578,57 @@ def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0,
     """owq_cache_attention: q [rows, query heads, head size], fp16 or bf16, over the pages; starts, lengths, page_table as for
     cache_append.  scale: 1 / sqrt(head size) if None.  max_new, max_len: the most rows and tokens of a sequence (defaults: all rows,
     the table's capacity; the work is split by these bounds).  Returns out, or (out, lse)."""
-    import torch
-    _heads(q, "q")
+    torch = _torch()
     rows, q_heads, dim = q.shape
-    n_seqs = lengths.numel()
-    desc = _cache_desc(pages, page_table, n_seqs, pages.shape[1], dim)
+    q_row, q_head, q1 = q.stride()
+    assert q.is_cuda and q1 == 1, q.shape
+    n_seqs, device = lengths.numel(), q.device
+    desc, most = _cache_args(pages, page_table, n_seqs, pages.shape[1], dim)
     if out is None:
-        out = torch.empty((rows, q_heads, dim), dtype=q.dtype, device=q.device)
+        out = torch.empty((rows, q_heads, dim), dtype=q.dtype, device=device)
     else:
-        assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.is_contiguous()
-    lse = torch.empty((rows, q_heads), dtype=torch.float32, device=q.device) if want_lse else None
-    most = desc.table_stride * desc.page_size
-    att = AttentionDesc(q_heads, _type_of(q), rows, rows if max_new is None else max_new, most if max_len is None else min(max_len, most),
-                        window, sinks, dim ** -0.5 if scale is None else scale, q.stride(0), q.stride(1))
+        assert out.shape == q.shape and out.dtype is q.dtype and out.is_cuda and out.is_contiguous()
+    lse = torch.empty((rows, q_heads), dtype=torch.float32, device=device) if want_lse else None
+    att = _ATTENTION.pack(q_heads, _type_of(q), rows, rows if max_new is None else max_new, most if max_len is None else min(max_len, most),
+                          window, sinks, dim ** -0.5 if scale is None else scale, q_row, q_head)
+    L = lib()
     if workspace is None:
-        n = owq_cache_attention_workspace_bytes(desc, att)
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-    owq_cache_attention(desc, att, q.data_ptr(), pages.data_ptr(), page_table.data_ptr(), _int32(starts, n_seqs + 1, "starts"),
-                        _int32(lengths, n_seqs, "lengths"), out.data_ptr(), lse.data_ptr() if want_lse else 0,
-                        workspace.data_ptr() if workspace is not None else 0, workspace.numel() if workspace is not None else 0,
-                        _current_stream(torch))
+        need = C.c_size_t(0)
+        status = L.owq_cache_attention_workspace_bytes(desc, att, need)
+        if status != OWQ_OK:
+            raise OwqError(status, "owq_cache_attention_workspace_bytes")
+        n = need.value
+        workspace = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    else:
+        n = workspace.numel()
+    status = L.owq_cache_attention(desc, att, q.data_ptr(), pages.data_ptr(), _int32(page_table, n_seqs, "page_table"),
+                                   _int32(starts, n_seqs + 1, "starts"), _int32(lengths, n_seqs, "lengths"), out.data_ptr(), _ptr_of(lse),
+                                   _ptr_of(workspace), n, _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_cache_attention")
     return (out, lse) if want_lse else out
 
 
 def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
     """owq_sample: logits [rows, vocabulary] (fp16, bf16 or fp32), noise fp32 [rows, vocabulary] exponential variates (None if every
     temperature is 0); temperature, top_p, min_p fp32 and top_k int32 [rows] or None.  Returns (token int32, log-probability fp32)."""
-    import torch
-    assert logits.dim() == 2 and logits.is_cuda and (logits.stride(1) == 1 or logits.shape[1] == 1)
+    torch = _torch()
     rows, vocab = logits.shape
+    row, one = logits.stride()
+    f32, device = torch.float32, logits.device
+    assert logits.is_cuda and (one == 1 or vocab == 1), logits.stride()
+    noise_row = 0
     if noise is not None:
-        assert noise.dtype == torch.float32 and noise.shape == logits.shape and noise.is_cuda and (noise.stride(1) == 1 or vocab == 1)
+        noise_row, one = noise.stride()
+        assert noise.is_cuda and noise.dtype is f32 and noise.shape == logits.shape and (one == 1 or vocab == 1), noise.shape
     for x in (temperature, top_p, min_p):
-        assert x is None or (x.dtype == torch.float32 and x.is_cuda and x.is_contiguous() and x.numel() == rows)
-    if top_k is not None:
-        _int32(top_k, rows, "top_k")
-    kind = _type_of(logits, f32=True)
-    token = torch.empty(rows, dtype=torch.int32, device=logits.device)
-    logprob = torch.empty(rows, dtype=torch.float32, device=logits.device)
-    n = owq_sample_workspace_bytes(rows, vocab, kind)
-    workspace = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
-    ptr = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
-    owq_sample(logits.data_ptr(), kind, rows, vocab, logits.stride(0), ptr(noise), 0 if noise is None else noise.stride(0), ptr(temperature),
-               ptr(top_k), ptr(top_p), ptr(min_p), token.data_ptr(), logprob.data_ptr(), ptr(workspace), n, _current_stream(torch))
+        assert x is None or (x.is_cuda and x.dtype is f32 and x.is_contiguous() and x.numel() == rows)
+    token, logprob = torch.empty(rows, dtype=torch.int32, device=device), torch.empty(rows, dtype=f32, device=device)
+    status = lib().owq_sample(logits.data_ptr(), _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, _ptr_of(noise), noise_row,
+                              _ptr_of(temperature), 0 if top_k is None else _int32(top_k, rows, "top_k"), _ptr_of(top_p), _ptr_of(min_p),
+                              token.data_ptr(), logprob.data_ptr(), _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_sample")
     return token, logprob
 
 

@@ -39,7 +39,8 @@ struct AttendArgs {
   const u32 *q;
   u32 *out;
   float *lse;
-  float *part;           // [sequence, head, row][split][P + 2]: sums of p s c + p lo, then ref, sum of p
+  float *part;           // [sequence, head, row][split][P]: sums of p s (c - 8) + p (lo + 8 s)
+  float *part_sums;      // [sequence, head, row][split][2]: reference, sum of p
   int64_t q_row, q_head;
   int32_t q_heads, group, rows, row_blocks, splits, tiles_per_split, window, sinks, max_len, bf16;
   float scale;           // log2 e included
@@ -263,6 +264,17 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &sp
   }
 }
 
+// Over the wave, in every lane, in a fixed order.
+__device__ __forceinline__ float wave_sum(float v) {
+  v = lanes_sum<16>(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+__device__ __forceinline__ float wave_max(float v) {
+  v = lanes_max<16>(v);
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
 __device__ __forceinline__ float quads_sum(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
@@ -410,12 +422,13 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : 4) void ow
     const int64_t at = (int64_t)row0 + row / a.group;
     if (at < 0 || at >= c.n_rows) continue;
     if (a.splits > 1) {
-      float *dst = a.part + ((((int64_t)b * c.kv_heads + head) * a.rows + row) * a.splits + split) * (P + 2);
+      const int64_t slot = (((int64_t)b * c.kv_heads + head) * a.rows + row) * a.splits + split;
+      float *dst = a.part + slot * P + part * 2 * STEPS;
 #pragma unroll
-      for (int e = 0; e < 2 * STEPS; ++e) dst[part * 2 * STEPS + e] = o[e];
+      for (int e = 0; e < 2 * STEPS; ++e) dst[e] = o[e];
       if (part == 0) {
-        dst[P] = ref;
-        dst[P + 1] = total;
+        a.part_sums[2 * slot] = ref;
+        a.part_sums[2 * slot + 1] = total;
       }
     } else {
       const int h = head * a.group + row % a.group;
@@ -431,7 +444,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : 4) void ow
   }
 }
 
-// The ranges of a row joined: one wave per row, 2 columns per lane.
+// The ranges of a row joined: one wave per row, two columns per lane, 16 ranges in flight.
 __global__ __launch_bounds__(256) void owq_attend_join_kernel(AttendArgs a, int block_rows, int P) {
   const CacheView &c = a.c;
   const int lane = threadIdx.x & 63;
@@ -447,21 +460,38 @@ __global__ __launch_bounds__(256) void owq_attend_join_kernel(AttendArgs a, int 
   const Span span = visible_tiles(a, len - n_new + first / a.group, len - n_new + last / a.group);
   int used = (span.count + a.tiles_per_split - 1) / a.tiles_per_split;
   used = used < 1 ? 1 : used;
-  const float *src = a.part + (((int64_t)b * c.kv_heads + head) * a.rows + row) * a.splits * (P + 2);
+  const int64_t slot = (((int64_t)b * c.kv_heads + head) * a.rows + row) * a.splits;
+  const float *sums = a.part_sums + 2 * slot, *src = a.part + slot * P;
   float ref = kNoRef;
-  for (int s = 0; s < used; ++s) ref = fmaxf(ref, src[(int64_t)s * (P + 2) + P]);
+  for (int s = lane; s < used; s += 64) ref = fmaxf(ref, sums[2 * s]);
+  ref = wave_max(ref);
   float total = 0.f, o0 = 0.f, o1 = 0.f;
-  const bool on = 2 * lane < c.head_dim;
-  for (int s = 0; s < used; ++s) {
-    const float *p = src + (int64_t)s * (P + 2);
-    const float f = __builtin_amdgcn_exp2f(p[P] - ref);
-    total = __builtin_fmaf(f, p[P + 1], total);
-    o0 = __builtin_fmaf(f, on ? p[2 * lane] : 0.f, o0);
-    o1 = __builtin_fmaf(f, on ? p[2 * lane + 1] : 0.f, o1);
+  const int col = 2 * lane < P ? 2 * lane : 0;
+  for (int base = 0; base < used; base += 64) {
+    const int mine = base + lane;
+    const float f = mine < used ? __builtin_amdgcn_exp2f(sums[2 * mine] - ref) : 0.f;
+    total = __builtin_fmaf(f, mine < used ? sums[2 * mine + 1] : 0.f, total);
+    const int n = used - base < 64 ? used - base : 64;
+    for (int s = 0; s < n; s += 16) {
+      float2 v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at_s = base + (s + i < n ? s + i : n - 1);
+        v[i] = *reinterpret_cast<const float2 *>(src + (int64_t)at_s * P + col);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        // lanes past the last range have f = 0
+        const float g = s + i < n ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (s + i) & 63)) : 0.f;
+        o0 = s + i < n ? __builtin_fmaf(g, v[i].x, o0) : o0;
+        o1 = s + i < n ? __builtin_fmaf(g, v[i].y, o1) : o1;
+      }
+    }
   }
+  total = wave_sum(total);
   const int h = head * a.group + row % a.group;
   const float inv = total == 0.f ? 0.f : 1.f / total;
-  if (on) a.out[(at * a.q_heads + h) * (c.head_dim / 2) + lane] = a.bf16 ? BF16::pack(o0 * inv, o1 * inv) : F16::pack(o0 * inv, o1 * inv);
+  if (2 * lane < c.head_dim) a.out[(at * a.q_heads + h) * (c.head_dim / 2) + lane] = a.bf16 ? BF16::pack(o0 * inv, o1 * inv) : F16::pack(o0 * inv, o1 * inv);
   if (a.lse != nullptr && lane == 0) a.lse[at * a.q_heads + h] = total == 0.f ? -__builtin_inff() : (ref + __builtin_log2f(total)) * 0.69314718056f;
 }
 
@@ -492,7 +522,8 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
     p.splits = std::max(1, (tiles + p.tiles_per_split - 1) / p.tiles_per_split);
   }
   const int P = (d.head_dim + 31) / 32 * 32;
-  p.workspace = p.splits > 1 ? (size_t)d.n_seqs * d.kv_heads * p.rows * p.splits * (P + 2) * 4 : 0;
+  p.slots = (size_t)d.n_seqs * d.kv_heads * p.rows * p.splits;
+  p.workspace = p.splits > 1 ? p.slots * (P + 2) * 4 : 0;
   return p;
 }
 
@@ -512,6 +543,7 @@ int launch_attend(const CacheView &c, const owq_attention_desc_t &d, const Atten
   a.out = static_cast<u32 *>(out);
   a.lse = lse;
   a.part = static_cast<float *>(workspace);
+  a.part_sums = a.part + p.slots * ((c.head_dim + 31) / 32 * 32);
   a.q_row = d.q_row, a.q_head = d.q_head;
   a.q_heads = d.q_heads, a.group = p.group, a.rows = p.rows, a.row_blocks = p.row_blocks, a.splits = p.splits;
   a.tiles_per_split = p.tiles_per_split, a.window = d.window, a.sinks = d.sinks, a.max_len = d.max_len;

@@ -193,20 +193,34 @@ __global__ __launch_bounds__(256) void owq_rope_backward_kernel(RopeArgs a) {
   }
 }
 
-// Column sums of partial [rows][2 dim]: 32 columns per workgroup, 32 rows at a time.
+// Column sums of partial [rows][2 dim]: 8 columns per workgroup, 128 rows at a time, eight of a thread's in flight.
 __global__ __launch_bounds__(1024) void owq_rope_weights_kernel(const float *partial, int rows, int dim, float *dwq, float *dwk) {
-  __shared__ float sums[32][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), first = threadIdx.x >> 5;
+  __shared__ float sums[128][9];
+  const int lane = threadIdx.x & 7, first = threadIdx.x >> 3;
+  const int col = blockIdx.x * 8 + lane;
   float v = 0.f;
-  if (col < 2 * dim)
-    for (int i = first; i < rows; i += 32) v += partial[(int64_t)i * 2 * dim + col];
-  sums[first][threadIdx.x & 31] = v;
+  if (rows > 0)
+    for (int base = 0; base < rows; base += 1024) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = base + 128 * j + first;
+        x[j] = partial[(int64_t)(i < rows ? i : rows - 1) * 2 * dim + col];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v += base + 128 * j + first < rows ? x[j] : 0.f;
+    }
+  sums[first][lane] = v;
   __syncthreads();
-  if (first == 0 && col < 2 * dim) {
+  if (threadIdx.x < 64) {            // eight threads a column, 16 rows each
+    const int c = threadIdx.x >> 3, part = threadIdx.x & 7;
     float total = 0.f;
-    for (int i = 0; i < 32; ++i) total += sums[i][threadIdx.x];
-    float *out = col < dim ? dwq : dwk;
-    if (out != nullptr) out[col < dim ? col : col - dim] = total;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) total += sums[16 * part + i][c];
+    total = lanes_sum<8>(total);
+    const int at = blockIdx.x * 8 + c;
+    float *out = at < dim ? dwq : dwk;
+    if (part == 0 && out != nullptr) out[at < dim ? at : at - dim] = total;
   }
 }
 
@@ -297,7 +311,7 @@ int launch_rope_backward(const owq_rope_desc_t &d, const RopePtrs &p, void *stre
     });
   });
   if (p.dwq != nullptr || p.dwk != nullptr)      // no tokens: zeros
-    owq_rope_weights_kernel<<<(2 * d.head_dim + 31) / 32, 1024, 0, static_cast<hipStream_t>(stream)>>>(a.partial, blocks, d.head_dim, p.dwq, p.dwk);
+    owq_rope_weights_kernel<<<2 * d.head_dim / 8, 1024, 0, static_cast<hipStream_t>(stream)>>>(a.partial, blocks, d.head_dim, p.dwq, p.dwk);
   return (int)hipGetLastError();
 }
 

@@ -584,9 +584,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   }
 }
 
-size_t sample_workspace(int32_t, int32_t, int32_t) { return 0; }
-
-int launch_sample(const SampleArgs &a, int32_t type, void *, void *stream) {
+int launch_sample(const SampleArgs &a, int32_t type, void *stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (type == OWQ_TYPE_F16) owq_sample_kernel<OWQ_TYPE_F16><<<a.n_rows, kSampleThreads, 0, s>>>(a);
   else if (type == OWQ_TYPE_BF16) owq_sample_kernel<OWQ_TYPE_BF16><<<a.n_rows, kSampleThreads, 0, s>>>(a);

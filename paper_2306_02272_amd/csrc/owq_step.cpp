@@ -180,17 +180,9 @@ static owq_status_t check_sample(int32_t n_rows, int32_t vocab, int32_t type) {
   return OWQ_OK;
 }
 
-owq_status_t owq_sample_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t type, size_t *bytes) {
-  const owq_status_t st = check_sample(n_rows, vocab, type);
-  if (st != OWQ_OK) return st;
-  if (!bytes) return OWQ_ERR_NULL;
-  *bytes = n_rows > 0 ? sample_workspace(n_rows, vocab, type) : 0;
-  return OWQ_OK;
-}
-
 owq_status_t owq_sample(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row, const float *noise,
                         int64_t noise_row, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
-                        int32_t *token, float *logprob, void *workspace, size_t workspace_bytes, void *stream) {
+                        int32_t *token, float *logprob, void *stream) {
   const owq_status_t st = check_sample(n_rows, vocab, type);
   if (st != OWQ_OK) return st;
   if (n_rows == 0) return OWQ_OK;
@@ -198,11 +190,8 @@ owq_status_t owq_sample(const void *logits, int32_t type, int32_t n_rows, int32_
   if (!aligned(logits, type == OWQ_TYPE_F32 ? 4 : 2) || !aligned(noise, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
       !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(token, 4) || !aligned(logprob, 4))
     return OWQ_ERR_BUFFER;
-  const size_t need = sample_workspace(n_rows, vocab, type);
-  if (need > 0 && !workspace) return OWQ_ERR_NULL;
-  if (need > 0 && (!aligned(workspace, 16) || workspace_bytes < need)) return OWQ_ERR_BUFFER;
   const SampleArgs a{logits, noise, temperature, top_p, min_p, top_k, token, logprob, logits_row, noise_row, n_rows, vocab};
-  return launch_sample(a, type, workspace, stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
+  return launch_sample(a, type, stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
 }
 
 }  // extern "C"

@@ -48,6 +48,7 @@ struct AttendPlan {
   int32_t row_blocks;   // workgroups along the rows
   int32_t splits;       // ranges of keys
   int32_t tiles_per_split;
+  size_t slots;         // partial results: rows x ranges
   size_t workspace;
 };
 AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a);
@@ -63,7 +64,6 @@ struct SampleArgs {
   int64_t logits_row, noise_row;
   int32_t n_rows, vocab;
 };
-size_t sample_workspace(int32_t n_rows, int32_t vocab, int32_t type);
-int launch_sample(const SampleArgs &a, int32_t type, void *workspace, void *stream);
+int launch_sample(const SampleArgs &a, int32_t type, void *stream);
 
 }  // namespace owq

@@ -136,11 +136,11 @@ def test_attention_workspace(lib):
 @pytest.mark.parametrize("rows,vocab,type,want", [(-1, 5, 0, B.OWQ_ERR_SHAPE), (2, 0, 0, B.OWQ_ERR_SHAPE), (2, (1 << 24) + 1, 0, B.OWQ_ERR_SHAPE),
                                                   (2, 5, 3, B.OWQ_ERR_TYPE), (0, 5, 0, B.OWQ_OK)])
 def test_sample(lib, rows, vocab, type, want):
-    assert status(B.owq_sample, P, type, rows, vocab, 5, P, 5, P, P, P, P, P, P, P, 1 << 20) == want
+    assert status(B.owq_sample, P, type, rows, vocab, 5, P, 5, P, P, P, P, P, P) == want
 
 
 def test_sample_pointers(lib):
-    good = dict(logits=P, type=2, rows=2, vocab=5, lrow=5, noise=P, nrow=5, t=P, k=P, p=P, m=P, token=P, lp=P, ws=P, n=1 << 20)
+    good = dict(logits=P, type=2, rows=2, vocab=5, lrow=5, noise=P, nrow=5, t=P, k=P, p=P, m=P, token=P, lp=P)
     call = lambda **kw: status(B.owq_sample, *{**good, **kw}.values())  # noqa: E731
     assert call(logits=0) == B.OWQ_ERR_NULL and call(token=0) == B.OWQ_ERR_NULL and call(noise=0, t=0) == B.OWQ_ERR_NULL
     for name in ("logits", "noise", "t", "k", "p", "m", "token", "lp"):

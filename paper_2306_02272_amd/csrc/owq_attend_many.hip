@@ -1,0 +1,60 @@
+// Attention over the 4-bit cache, many rows per sequence and key/value head: prompts.  The waves of a workgroup take other
+// rows of the same keys, whose words they find in the caches.
+#include <hip/hip_runtime.h>
+
+#include "owq_attend_device.h"
+
+namespace owq {
+
+constexpr int kCols = 2;       // 16-row tiles of a wave
+
+template <int STEPS>
+__global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendArgs a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int quad = lane >> 4, col = lane & 15;
+  const int head = blockIdx.y, b = blockIdx.z;
+  const Sequence sq = sequence_of(a, b);
+  const int first = (blockIdx.x * kWaves + wave) * 16 * kCols;
+  if (first >= sq.n_rows) return;
+  const int last = (first + 16 * kCols < sq.n_rows ? first + 16 * kCols : sq.n_rows) - 1;
+  const int pa = sq.p0 + first / a.group, pb = sq.p0 + last / a.group;
+  const Span span = visible_tiles(a, pa, pb);
+  Rows<STEPS, kCols> w;
+  attend_span<1>(a, sq, span, b, head, first, pa, pb, 0, span.count, 0, lane, w);
+#pragma unroll
+  for (int n = 0; n < kCols; ++n) {
+    const float l = quads_sum(w.l[n]), low = quads_sum(w.low[n]);
+    const int row = first + 16 * n + col;
+    const int token = row / a.group;
+    const int64_t at = (int64_t)sq.row0 + token;
+    if (row >= sq.n_rows || at < 0 || at >= a.c.n_rows) continue;
+    const int h = head * a.group + row - token * a.group;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    u32 *out = a.out + (at * a.q_heads + h) * (a.c.head_dim / 2);
+#pragma unroll
+    for (int d = 0; d < 2 * STEPS; ++d) {
+      const int dim = 16 * d + 4 * quad;
+      if (dim >= a.c.head_dim) continue;
+      float o[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r], 0x1p20f, low) * inv;
+      *reinterpret_cast<u32x2 *>(out + dim / 2) =
+          a.bf16 ? (u32x2){BF16::pack(o[0], o[1]), BF16::pack(o[2], o[3])} : (u32x2){F16::pack(o[0], o[1]), F16::pack(o[2], o[3])};
+    }
+    if (a.lse != nullptr && quad == 0) a.lse[at * a.q_heads + h] = lse_of(w.ref[n], l);
+  }
+}
+
+template <int STEPS>
+void launch_attend_many(const AttendArgs &a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.max_new * a.group;
+  constexpr int block = 16 * kCols * kWaves;
+  const dim3 grid((unsigned)((rows + block - 1) / block), (unsigned)a.c.kv_heads, (unsigned)a.c.n_seqs);
+  owq_attend_many_kernel<STEPS><<<grid, 64 * kWaves, 0, stream>>>(a);
+}
+template void launch_attend_many<1>(const AttendArgs &, hipStream_t);
+template void launch_attend_many<2>(const AttendArgs &, hipStream_t);
+template void launch_attend_many<3>(const AttendArgs &, hipStream_t);
+template void launch_attend_many<4>(const AttendArgs &, hipStream_t);
+
+}  // namespace owq

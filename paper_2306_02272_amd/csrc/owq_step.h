@@ -42,13 +42,12 @@ int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type
 // The work split of an attention call: everything that follows from the description alone.
 struct AttendPlan {
   int32_t group;        // query heads per key/value head
-  int32_t rows;         // most rows (new tokens x group) of a sequence and key/value head
-  int32_t col_tiles;    // 16-row tiles of a wave
-  bool share_keys;      // the waves of a workgroup take other rows of the same keys (else other keys of the same rows)
-  int32_t row_blocks;   // workgroups along the rows
-  int32_t splits;       // ranges of keys
-  int32_t tiles_per_split;
-  size_t slots;         // partial results: rows x ranges
+  int32_t rows;         // few rows: most rows (new tokens x group) of a sequence and key/value head
+  bool many;            // more than 64 of them
+  int32_t col_tiles;    // few: 16-row tiles of a wave
+  bool whole;           // few: one workgroup per sequence and head
+  int32_t ranges, least_tiles, workgroups;
+  size_t slots;         // rows of partial results
   size_t workspace;
 };
 AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a);

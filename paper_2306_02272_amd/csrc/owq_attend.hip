@@ -11,12 +11,7 @@
 
 namespace owq {
 
-typedef unsigned long long u64;
-
-#ifndef RESIDENT
-#define RESIDENT 4
-#endif
-constexpr int kResident = RESIDENT;      // workgroups of one column tile that a compute unit holds
+constexpr int kResident = 3;      // workgroups of one column tile that a compute unit holds
 
 // Tiles of each of a sequence's heads, at least one where there are rows, so that rows that see nothing are written.
 __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Sequence &sq) {
@@ -26,48 +21,30 @@ __device__ __forceinline__ int tiles_of(const AttendArgs &a, const Sequence &sq)
 }
 __device__ __forceinline__ int tiles_of(const AttendArgs &a, int b) { return b < a.c.n_seqs ? tiles_of(a, sequence_of(a, b)) : 0; }
 
-struct RangeShared {
-  u64 part[kWaves];
-  int seq, place, tiles, ranges;
-  Sequence sq;
-};
-
-__device__ __forceinline__ u64 wave_scan64(u64 v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const u64 o = __shfl_up(v, s);
-    v += lane >= s ? o : 0ull;
-  }
-  return v;
-}
-__device__ __forceinline__ u64 block_sum64(u64 v, RangeShared &sh) {
-  v = wave_scan64(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) sh.part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) v += sh.part[w];
-  return v;
+__device__ __forceinline__ u64 add64(u64 a, u64 b) { return a + b; }
+__device__ __forceinline__ u64 last_lane(u64 v) {
+  return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (u32)__builtin_amdgcn_readlane((int)v, 63);
 }
 
-// Most tiles of a range: `ranges` of them over all heads, or as many more as it takes that every head has one.  Two
-// corrections bring their number near `ranges` where that can be.  `mine` = the tiles of sequence threadIdx.x.
-__device__ __forceinline__ int range_length(const AttendArgs &a, int mine, RangeShared &sh) {
-  constexpr int kAll = 64 * kWaves;
-  u64 total = (u64)mine;
-  for (int b = threadIdx.x + kAll; b < a.c.n_seqs; b += kAll) total += tiles_of(a, b);
-  total = block_sum64(total, sh) * a.c.kv_heads;
-  const u64 want = (u64)a.ranges;
+// f(sequence's tiles) summed over all sequences, by every wave for itself: no barriers.  `mine` = the tiles of sequence `lane`.
+template <class F>
+__device__ __forceinline__ u64 sum_over(const AttendArgs &a, int mine, int lane, F &&f) {
+  u64 v = f(mine);
+  for (int b = lane + 64; b < a.c.n_seqs; b += 64) v += f(tiles_of(a, b));
+  return last_lane(wave_scan(v, (u64)0, add64));
+}
+
+// Most tiles of a range: a.ranges of them over all heads, or as many more as it takes that every head has one.  Two
+// corrections bring their number to a.ranges or below where that can be.
+__device__ __forceinline__ int range_length(const AttendArgs &a, int mine, int lane) {
+  const u64 want = (u64)a.ranges, heads = (u64)a.c.kv_heads;
+  const u64 total = sum_over(a, mine, lane, [](int n) { return (u64)n; }) * heads;
   u64 length = (total + want - 1) / want;
   length = length > (u64)a.least_tiles ? length : (u64)a.least_tiles;
-  if ((u64)a.c.n_seqs * a.c.kv_heads * 2 <= want)
+  if ((u64)a.c.n_seqs * heads * 2 <= want && a.c.n_seqs > 1)
     for (int k = 0; k < 2; ++k) {
       const int l = (int)length;
-      u64 n = (u64)((mine + l - 1) / l);
-      for (int b = threadIdx.x + kAll; b < a.c.n_seqs; b += kAll) n += (tiles_of(a, b) + l - 1) / l;
-      n = block_sum64(n, sh) * a.c.kv_heads;
+      const u64 n = sum_over(a, mine, lane, [&](int t) { return (u64)((t + l - 1) / l); }) * heads;
       if (n <= want) break;
       length = (length * n + want - 1) / want;
     }
@@ -95,56 +72,46 @@ template <int STEPS, int NQ>
 __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
   constexpr int P = 32 * STEPS;
   __shared__ float red[kWaves][16][P + 4];
-  __shared__ RangeShared sh;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quad = lane >> 4, col = lane & 15;
 
-  // this workgroup's sequence, head and range
+  // this workgroup's sequence, head and range: every wave finds them for itself
+  Sequence sq = {0, 0, 0};
+  int b = -1, place = 0, ranges = 0;
   {
-    const Sequence sq = (int)threadIdx.x < a.c.n_seqs ? sequence_of(a, threadIdx.x) : Sequence{0, 0, 0};
-    const int mine = tiles_of(a, sq);
-    const int length = a.whole ? 0x7fffffff : range_length(a, mine, sh);
-    if (threadIdx.x == 0) sh.seq = -1;
+    Sequence mine = {0, 0, 0};
+    if (lane < a.c.n_seqs) mine = sequence_of(a, lane);
+    int tiles = tiles_of(a, mine);
+    const int length = a.whole ? 0x7fffffff : range_length(a, tiles, lane);
     u64 before = 0;
-    for (int base = 0; base < a.c.n_seqs; base += 64 * kWaves) {
-      const int b = base + threadIdx.x;
-      const Sequence q = base == 0 ? sq : b < a.c.n_seqs ? sequence_of(a, b) : Sequence{0, 0, 0};
-      const int tiles = base == 0 ? mine : tiles_of(a, q);
-      const int ranges = tiles > 0 ? (tiles - 1) / length + 1 : 0;
-      const u64 cost = (u64)ranges * a.c.kv_heads;
-      const u64 scan = wave_scan64(cost);
-      __syncthreads();
-      if (lane == 63) sh.part[wave] = scan;
-      __syncthreads();
-      u64 from = before + scan - cost;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        from += w < wave ? sh.part[w] : 0ull;
-        before += sh.part[w];
+    for (int base = 0; base < a.c.n_seqs; base += 64) {
+      if (base > 0) {
+        mine = base + lane < a.c.n_seqs ? sequence_of(a, base + lane) : Sequence{0, 0, 0};
+        tiles = tiles_of(a, mine);
       }
-      if (from <= blockIdx.x && blockIdx.x < from + cost) {
-        sh.seq = b;
-        sh.place = (int)(blockIdx.x - from);
-        sh.tiles = tiles;
-        sh.ranges = ranges;
-        sh.sq = q;
-        if (!a.whole && from == blockIdx.x) {       // for the second launch
-          a.places[2 * b] = (int)from;
-          a.places[2 * b + 1] = ranges;
-        }
+      const int own = tiles > 0 ? (tiles - 1) / length + 1 : 0;
+      const u64 cost = (u64)own * a.c.kv_heads;
+      const u64 scan = wave_scan(cost, (u64)0, add64), from = before + scan - cost;
+      const u64 here = __ballot(from <= blockIdx.x && blockIdx.x < from + cost);
+      if (here != 0) {
+        const int l = __ffsll(here) - 1;
+        b = base + l;
+        place = __builtin_amdgcn_readlane((int)(blockIdx.x - from), l);
+        ranges = __builtin_amdgcn_readlane(own, l);
+        sq.row0 = __builtin_amdgcn_readlane(mine.row0, l);
+        sq.n_rows = __builtin_amdgcn_readlane(mine.n_rows, l);
+        sq.p0 = __builtin_amdgcn_readlane(mine.p0, l);
+        break;
       }
-      if (before > blockIdx.x) break;         // uniform
+      before += last_lane(scan);
     }
-    __syncthreads();
   }
-  const int b = __builtin_amdgcn_readfirstlane(sh.seq);
   if (b < 0) return;
-  const int ranges = __builtin_amdgcn_readfirstlane(sh.ranges), place = __builtin_amdgcn_readfirstlane(sh.place);
+  if (!a.whole && place == 0 && threadIdx.x == 0) {       // for the second launch
+    a.places[2 * b] = (int)blockIdx.x;
+    a.places[2 * b + 1] = ranges;
+  }
   const int head = place / ranges, range = place - head * ranges;
-  Sequence sq;
-  sq.row0 = __builtin_amdgcn_readfirstlane(sh.sq.row0);
-  sq.n_rows = __builtin_amdgcn_readfirstlane(sh.sq.n_rows);
-  sq.p0 = __builtin_amdgcn_readfirstlane(sh.sq.p0);
   const int pa = sq.p0, pb = sq.p0 + (sq.n_rows - 1) / a.group;
   const Span span = visible_tiles(a, pa, pb);
   const int i0 = (int)((int64_t)span.count * range / ranges), i1 = (int)((int64_t)span.count * (range + 1) / ranges);
@@ -252,7 +219,7 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   // as many workgroups as the compute units hold at once (of four waves, by registers), two tiles per wave at least;
   // where no sequence has more than four tiles per wave, whole items and no joining
   const int64_t resident = 256 * (p.col_tiles == 4 ? 1 : p.col_tiles == 2 ? 2 : kResident);
-  p.whole = tiles <= 4 * 4;
+  p.whole = tiles <= 4 * 4 || (items >= 256 && tiles <= 16 * 4);
   p.least_tiles = 2 * 4;
   // heads that fill the compute units by themselves come in turns, and twice the ranges even out their lengths
   p.ranges = (int)(2 * items <= resident ? resident : 2 * resident);

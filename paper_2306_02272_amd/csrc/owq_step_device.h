@@ -10,6 +10,7 @@ namespace owq {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef u32 u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned long long u64;
 
 struct F16 {
   static __device__ __forceinline__ float lo(u32 w) { return half_lo(w); }
@@ -66,6 +67,33 @@ __device__ __forceinline__ float lanes_max(float v) {
   if (L >= 8) v = fmaxf(v, dpp<0x141>(v));
   if (L >= 16) v = fmaxf(v, dpp<0x140>(v));
   return v;
+}
+
+// A value from another lane of the wave, `none` where there is no such lane: the six steps of a scan over 64 lanes
+// (1, 2, 4 and 8 lanes down within rows of 16, then the last lane of a row to the next row, and of the lower half to the upper).
+template <int STEP>
+__device__ __forceinline__ u32 from_lane(u32 v, u32 none) {
+  constexpr int ctrl = STEP == 0 ? 0x111 : STEP == 1 ? 0x112 : STEP == 2 ? 0x114 : STEP == 3 ? 0x118 : STEP == 4 ? 0x142 : 0x143;
+  constexpr int rows = STEP == 4 ? 0xa : STEP == 5 ? 0xc : 0xf;
+  return (u32)__builtin_amdgcn_update_dpp((int)none, (int)v, ctrl, rows, 0xf, false);
+}
+template <int STEP>
+__device__ __forceinline__ u64 from_lane(u64 v, u64 none) {
+  return (u64)from_lane<STEP>((u32)(v >> 32), (u32)(none >> 32)) << 32 | from_lane<STEP>((u32)v, (u32)none);
+}
+template <int STEP>
+__device__ __forceinline__ float from_lane(float v, float none) {
+  return __builtin_bit_cast(float, from_lane<STEP>(__builtin_bit_cast(u32, v), __builtin_bit_cast(u32, none)));
+}
+// Inclusive scan over the wave's lanes; the last lane holds the result over all of them.
+template <class T, class F>
+__device__ __forceinline__ T wave_scan(T v, T none, F &&f) {
+  v = f(v, from_lane<0>(v, none));
+  v = f(v, from_lane<1>(v, none));
+  v = f(v, from_lane<2>(v, none));
+  v = f(v, from_lane<3>(v, none));
+  v = f(v, from_lane<4>(v, none));
+  return f(v, from_lane<5>(v, none));
 }
 
 }  // namespace owq

@@ -12,9 +12,13 @@ template <int STEPS>
 __global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quad = lane >> 4, col = lane & 15;
-  const int head = blockIdx.y, b = blockIdx.z;
+  // Causal rows see ever more keys: of the workgroups that share a compute unit (256 apart, where there are two), one comes
+  // from the front and one from the back.
+  u32 id = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+  if ((id & 256u) && (id | 255u) < gridDim.x * gridDim.y * gridDim.z) id ^= 255u;
+  const int block_x = id % gridDim.x, head = id / gridDim.x % gridDim.y, b = id / gridDim.x / gridDim.y;
   const Sequence sq = sequence_of(a, b);
-  const int first = (blockIdx.x * kWaves + wave) * 16 * kCols;
+  const int first = (block_x * kWaves + wave) * 16 * kCols;
   if (first >= sq.n_rows) return;
   const int last = (first + 16 * kCols < sq.n_rows ? first + 16 * kCols : sq.n_rows) - 1;
   const int pa = sq.p0 + first / a.group, pb = sq.p0 + last / a.group;

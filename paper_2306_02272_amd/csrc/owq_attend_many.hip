@@ -9,14 +9,17 @@ namespace owq {
 constexpr int kCols = 2;       // 16-row tiles of a wave
 
 template <int STEPS>
-__global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendArgs a, bool paired) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quad = lane >> 4, col = lane & 15;
   // Causal rows see ever more keys: of the workgroups that share a compute unit (256 apart, where there are two), one comes
   // from the front and one from the back.
-  u32 id = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
-  if ((id & 256u) && (id | 255u) < gridDim.x * gridDim.y * gridDim.z) id ^= 255u;
-  const int block_x = id % gridDim.x, head = id / gridDim.x % gridDim.y, b = id / gridDim.x / gridDim.y;
+  int block_x = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  if (paired) {
+    u32 id = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+    if ((id & 256u) && (id | 255u) < gridDim.x * gridDim.y * gridDim.z) id ^= 255u;
+    block_x = id % gridDim.x, head = id / gridDim.x % gridDim.y, b = id / gridDim.x / gridDim.y;
+  }
   const Sequence sq = sequence_of(a, b);
   const int first = (block_x * kWaves + wave) * 16 * kCols;
   if (first >= sq.n_rows) return;
@@ -54,7 +57,8 @@ void launch_attend_many(const AttendArgs &a, hipStream_t stream) {
   const int64_t rows = (int64_t)a.max_new * a.group;
   constexpr int block = 16 * kCols * kWaves;
   const dim3 grid((unsigned)((rows + block - 1) / block), (unsigned)a.c.kv_heads, (unsigned)a.c.n_seqs);
-  owq_attend_many_kernel<STEPS><<<grid, 64 * kWaves, 0, stream>>>(a);
+  const bool paired = (int64_t)grid.x * grid.y * grid.z < (1ll << 31);
+  owq_attend_many_kernel<STEPS><<<grid, 64 * kWaves, 0, stream>>>(a, paired);
 }
 template void launch_attend_many<1>(const AttendArgs &, hipStream_t);
 template void launch_attend_many<2>(const AttendArgs &, hipStream_t);

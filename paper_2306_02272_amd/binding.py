@@ -487,8 +487,7 @@ def qk_norm_rope(q, k, cos, sin, positions, wq=None, wk=None, eps=1e-6, interlea
     weights or None.  Returns (q, k) turned, packed; `out` = a pair of packed tensors to write to (the inputs' own if packed)."""
     desc, tokens = _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved)
     if out is None:
-        empty, dtype, device = _TORCH.empty, q.dtype, q.device
-        q_out, k_out = empty(q.shape, dtype=dtype, device=device), empty(k.shape, dtype=dtype, device=device)
+        q_out, k_out = q.new_empty(q.shape), k.new_empty(k.shape)      # half of torch.empty's time
     else:
         q_out, k_out = out
         for o, x in ((q_out, q), (k_out, k)):
@@ -504,16 +503,16 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, cos, sin, positions, wq=None, wk
     """owq_qk_norm_rope_backward: gradients of qk_norm_rope's outputs to those of q, k and, fp32, of the weights (None without one).
     q, k: the forward's inputs (read only where there is a weight).  Returns (dq, dk, dwq, dwk)."""
     desc, tokens = _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq_out, dk_out)
-    empty, dtype, device, dim = _TORCH.empty, q.dtype, q.device, q.shape[2]
-    dq, dk = empty(q.shape, dtype=dtype, device=device), empty(k.shape, dtype=dtype, device=device)
-    dwq = None if wq is None else empty(dim, dtype=_TORCH.float32, device=device)
-    dwk = None if wk is None else empty(dim, dtype=_TORCH.float32, device=device)
+    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
+    f32 = _TORCH.float32
+    dwq = None if wq is None else q.new_empty(q.shape[2], dtype=f32)
+    dwk = None if wk is None else q.new_empty(q.shape[2], dtype=f32)
     n = 0
     if wq is not None or wk is not None:
         if workspace is None:
             need = C.c_size_t(0)
             _check(lib().owq_qk_norm_rope_backward_workspace_bytes(desc, C.byref(need)), "owq_qk_norm_rope_backward_workspace_bytes")
-            workspace = empty(need.value, dtype=_TORCH.uint8, device=device)
+            workspace = q.new_empty(need.value, dtype=_TORCH.uint8)
         n = workspace.numel()
     status = lib().owq_qk_norm_rope_backward(desc, dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), _ptr_of(wq), _ptr_of(wk),
                                              cos.data_ptr(), sin.data_ptr(), _int32(positions, tokens, "positions"), dq.data_ptr(),
@@ -560,11 +559,11 @@ def cache_read(pages, page_table, starts, n_rows, head_dim, max_len=None, dtype=
     """owq_cache_read: tokens 0 .. starts[b + 1] - starts[b] - 1 of every sequence as (k, v) [n_rows, key/value heads, head_dim]."""
     torch = _torch()
     n_seqs = starts.numel() - 1
-    heads, device = pages.shape[1], pages.device
+    heads = pages.shape[1]
     desc, _ = _cache_args(pages, page_table, n_seqs, heads, head_dim)
     dtype = torch.float16 if dtype is None else dtype
     shape = (n_rows, heads, head_dim)
-    k, v = torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)
+    k, v = pages.new_empty(shape, dtype=dtype), pages.new_empty(shape, dtype=dtype)
     status = lib().owq_cache_read(desc, pages.data_ptr(), _int32(page_table, n_seqs, "page_table"), _int32(starts, n_seqs + 1, "starts"),
                                   k.data_ptr(), v.data_ptr(), _type_of(k), n_rows, n_rows if max_len is None else max_len,
                                   _current_stream(torch))
@@ -582,13 +581,13 @@ def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0,
     rows, q_heads, dim = q.shape
     q_row, q_head, q1 = q.stride()
     assert q.is_cuda and q1 == 1, q.shape
-    n_seqs, device = lengths.numel(), q.device
+    n_seqs = lengths.numel()
     desc, most = _cache_args(pages, page_table, n_seqs, pages.shape[1], dim)
     if out is None:
-        out = torch.empty((rows, q_heads, dim), dtype=q.dtype, device=device)
+        out = q.new_empty((rows, q_heads, dim))
     else:
         assert out.shape == q.shape and out.dtype is q.dtype and out.is_cuda and out.is_contiguous()
-    lse = torch.empty((rows, q_heads), dtype=torch.float32, device=device) if want_lse else None
+    lse = q.new_empty((rows, q_heads), dtype=torch.float32) if want_lse else None
     att = _ATTENTION.pack(q_heads, _type_of(q), rows, rows if max_new is None else max_new, most if max_len is None else min(max_len, most),
                           window, sinks, dim ** -0.5 if scale is None else scale, q_row, q_head)
     L = lib()
@@ -598,7 +597,7 @@ def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0,
         if status != OWQ_OK:
             raise OwqError(status, "owq_cache_attention_workspace_bytes")
         n = need.value
-        workspace = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+        workspace = q.new_empty(n, dtype=torch.uint8) if n else None
     else:
         n = workspace.numel()
     status = L.owq_cache_attention(desc, att, q.data_ptr(), pages.data_ptr(), _int32(page_table, n_seqs, "page_table"),
@@ -615,7 +614,7 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
     torch = _torch()
     rows, vocab = logits.shape
     row, one = logits.stride()
-    f32, device = torch.float32, logits.device
+    f32 = torch.float32
     assert logits.is_cuda and (one == 1 or vocab == 1), logits.stride()
     noise_row = 0
     if noise is not None:
@@ -623,7 +622,7 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
         assert noise.is_cuda and noise.dtype is f32 and noise.shape == logits.shape and (one == 1 or vocab == 1), noise.shape
     for x in (temperature, top_p, min_p):
         assert x is None or (x.is_cuda and x.dtype is f32 and x.is_contiguous() and x.numel() == rows)
-    token, logprob = torch.empty(rows, dtype=torch.int32, device=device), torch.empty(rows, dtype=f32, device=device)
+    token, logprob = logits.new_empty(rows, dtype=torch.int32), logits.new_empty(rows, dtype=f32)
     status = lib().owq_sample(logits.data_ptr(), _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, _ptr_of(noise), noise_row,
                               _ptr_of(temperature), 0 if top_k is None else _int32(top_k, rows, "top_k"), _ptr_of(top_p), _ptr_of(min_p),
                               token.data_ptr(), logprob.data_ptr(), _current_stream(torch))

@@ -523,8 +523,8 @@ owq_status_t owq_cache_attention(const owq_cache_desc_t *desc, const owq_attenti
  * if temperature is given, and is read at tokens that stay only.
  * logprob[row] (may be NULL) = z[token] - ln sum exp z over the whole vocabulary (with
  * temperature 1 where it is 0).  Logits of -infinity are never chosen.  A row whose largest
- * logit is not finite, or that has a NaN in it, or whose temperature is negative or NaN, has no
- * token: -1 and NaN; so has a row whose temperature is not 0 without noise.
+ * logit is not finite, or that has a NaN in it, or whose temperature is negative, NaN, infinite or
+ * below 2^-126, has no token: -1 and NaN; so has a row whose temperature is not 0 without noise.
  * Probabilities are summed as integers, in units of 2^-31 of the largest, so no order of summation shows.
  * n_rows == 0 is a no-op; vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
  */

@@ -184,7 +184,7 @@ def attention(q, pages, table, starts, lengths, scale, window=0, sinks=0):
 def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """-> (token, log-probability)."""
     x = np.asarray(logits, np.float64)
-    if np.isnan(x).any() or not np.isfinite(x.max()) or not t >= 0 or (t > 0 and noise is None):
+    if np.isnan(x).any() or not np.isfinite(x.max()) or not 0 <= t < math.inf or 0 < t < 2.0 ** -126 or (t > 0 and noise is None):
         return -1, math.nan
     z = x / (t if t > 0 else 1.0)
     total = z.max() + math.log(np.exp(z - z.max()).sum())

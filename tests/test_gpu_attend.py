@@ -85,6 +85,29 @@ def test_attention(env, case):
     check(env, out, lse, want, bf16)
 
 
+LONG = [  # many sequences, ranges of keys over several of them, more ranges of a head than lanes
+    ([3000, 700, 64, 2000], [1, 2, 0, 3], 8, 4, 64, 64, 0, 0, False), ([1] + [13 * b % 800 for b in range(149)], [1] * 150, 2, 1, 32, 32, 0, 0, False),
+    ([30000], [1], 1, 1, 32, 256, 0, 0, True), ([4000, 3000], [20, 1], 3, 1, 64, 32, 0, 0, False), ([5000, 40], [2, 2], 2, 1, 128, 64, 2200, 70, False),
+    ([600 + 2 * b for b in range(70)], [b % 3 for b in range(70)], 4, 4, 32, 32, 400, 3, False),
+    ([900, 1100], [700, 5], 2, 1, 32, 32, 0, 0, False), ([130] * 3, [129] * 3, 5, 5, 48, 64, 50, 0, True),
+]
+
+
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "%d sequences to %d, %d rows" % (len(c[0]), max(c[0]), max(c[1])))
+def test_long_and_many(env, case):
+    torch, B = env
+    lengths, news, hq, hk, dim, page, window, sinks, bf16 = case
+    lengths = [max(a, b) for a, b in zip(lengths, news)]
+    rng = np.random.default_rng(len(lengths) + hq)
+    pages, table = filled(env, rng, lengths, hk, dim, page)
+    starts = np.cumsum([0] + news)
+    q = torch.from_numpy(rng.normal(size=(int(starts[-1]), hq, dim))).to(torch.bfloat16 if bf16 else torch.float16).cuda()
+    out, lse = B.cache_attention(q, pages, i32(torch, table), i32(torch, starts), i32(torch, lengths), window=window, sinks=sinks,
+                                 max_new=max(news), max_len=max(lengths), want_lse=True)
+    want = step.attention(q.double().cpu().numpy(), pages.cpu().numpy(), table, starts, lengths, dim ** -0.5, window, sinks)
+    check(env, out, lse, want, bf16)
+
+
 @pytest.mark.parametrize("q_scale,v_scale", [(1e-4, 1.0), (40.0, 1.0), (1.0, 1e-6), (1.0, 3000.0), (0.0, 1.0)])
 @pytest.mark.parametrize("new", [1, 90])
 def test_magnitudes(env, q_scale, v_scale, new):

@@ -85,6 +85,7 @@ def test_masked_and_hopeless_rows(env):
     x[5, :4098] = -float("inf")
     x[6] = -65504
     check(env, x, e, top_k=[200, 5, 5, 5, 5, 5, 9, 0, 0], top_p=[0.9] * 7 + [1.0, 1.0], temperature=[1, 1, 1, 1, 1, 1, 1, -1.0, float("nan")])
+    check(env, x[4:9], e[4:9], temperature=[float("inf"), 1e-40, 2.0 ** -126, 1e30, 1e-3], top_p=[0.5] * 5)
     check(env, x[:7], None, temperature=[0.0] * 7)
     check(env, x[:2], None, temperature=[0.0, 1.0])
 

@@ -187,7 +187,7 @@ def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if np.isnan(x).any() or not np.isfinite(x.max()) or not 0 <= t < math.inf or 0 < t < 2.0 ** -126 or (t > 0 and noise is None):
         return -1, math.nan
     z = x / (t if t > 0 else 1.0)
-    total = z.max() + math.log(np.exp(z - z.max()).sum())
+    total = math.log(np.exp(z - z.max()).sum())          # beside the largest: it may be many times that
     order = np.argsort(-x, kind="stable")
     order = order[x[order] > -np.inf]
     token = order[0]
@@ -206,4 +206,4 @@ def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
         with np.errstate(divide="ignore"):
             score = z[order] - np.log(np.asarray(noise, np.float64)[order])
         token = order[score == score.max()].min()
-    return int(token), float(z[token] - total)
+    return int(token), float(z[token] - z.max() - total)

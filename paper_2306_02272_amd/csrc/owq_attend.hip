@@ -127,7 +127,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident)
     for (int d = 0; d < 2 * STEPS; ++d) {
       f32x4 o;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r], 0x1p20f, low);
+      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r] - w.mid[n][r], 0x1p20f, low);
       *reinterpret_cast<f32x4 *>(&red[wave][col][16 * d + 4 * quad]) = o;
     }
     if (quad == 0) {

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendA
       if (dim >= a.c.head_dim) continue;
       float o[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r], 0x1p20f, low) * inv;
+      for (int r = 0; r < 4; ++r) o[r] = __builtin_fmaf(w.acc[n][d][r] - w.mid[n][r], 0x1p20f, low) * inv;
       *reinterpret_cast<u32x2 *>(out + dim / 2) =
           a.bf16 ? (u32x2){BF16::pack(o[0], o[1]), BF16::pack(o[2], o[3])} : (u32x2){F16::pack(o[0], o[1]), F16::pack(o[2], o[3])};
     }

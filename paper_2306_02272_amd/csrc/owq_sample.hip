@@ -5,10 +5,9 @@
 //   top-k up to 512: the k-th of the 1024 threads' largest logits lies at or below the row's k-th, so that a little more
 //     than k logits are candidates; they are listed in LDS and each counts what precedes it, and the mass of that, which
 //     decides top-k and top-p at once.  Two passes over the row;
-//   top-p alone: masses are added up by bins of 1/128 in log2; the logits of the bin in which the wanted mass is reached
-//     are listed and ranked in the same way.  Three passes.
-// What does not fit those (larger k, a bin with more than 1024 logits as in flat rows) takes the general way: keys by four
-// histograms of eight bits each.  Passes are rolled loops of 16 logits per thread: with the row in registers every pass is
+//   a longer top-k, and top-p without a short one: counts, or masses, are added up by bins of 1/128 in log2; the logits of
+//     the bin in which the wanted sum is reached are listed and ranked in the same way.  Three passes for either.
+// A bin with more than 1024 logits, as in flat rows, takes the general way: keys by four histograms of eight bits each.  Passes are rolled loops of 16 logits per thread: with the row in registers every pass is
 // straight-line code that a launch runs through once, and its instructions come from memory more slowly than the row does
 // (179 us for 256 rows of 50 272 fp32 logits so).
 // Masses are 2^31 e^(z - max z) as integers, so that no order of additions shows.
@@ -345,6 +344,41 @@ __device__ __forceinline__ void precede(const u64 *list, const u32 *list_mass, u
   *mass = m;
 }
 
+// The first bin with which the sum over sh.mass reaches `want` (left in sh.digit; sh.total = the sum before it), or
+// 0xffffffff if there is none.
+__device__ __forceinline__ u32 find_bin(double want, SampleShared &sh) {
+  constexpr int kEach = kMassBins / kSampleThreads;
+  u64 own[kEach], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) sum += own[j] = sh.mass[threadIdx.x * kEach + j];
+  const u64 mine = sum;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  sum = wave_scan(sum, (u64)0, [](u64 a, u64 b) { return a + b; });
+  if (lane == 63) sh.wave_mass[wave] = sum;
+  if (threadIdx.x == 0) sh.digit = 0xffffffffu;
+  __syncthreads();
+  u64 ahead = sum - mine;
+  for (int w = 0; w < wave; ++w) ahead += sh.wave_mass[w];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) {
+    if ((double)ahead < want && (double)(ahead + own[j]) >= want) {
+      sh.digit = threadIdx.x * kEach + j;
+      sh.total = ahead;
+    }
+    ahead += own[j];
+  }
+  __syncthreads();
+  return sh.digit;
+}
+__device__ __forceinline__ void clear_bins(SampleShared &sh) {
+#pragma unroll
+  for (int j = 0; j < kMassBins / kSampleThreads; ++j) sh.mass[j * kSampleThreads + threadIdx.x] = 0;
+}
+__device__ __forceinline__ void clear_lists(SampleShared &sh) {
+  if (threadIdx.x == 0) sh.n_sure = sh.n_list = 0;
+  sh.list[threadIdx.x] = 0;
+}
+
 template <int TYPE>
 __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a) {
   __shared__ SampleShared sh;
@@ -360,12 +394,11 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   const int k = a.top_k ? a.top_k[r] : 0;
   const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
   const float top = block_top(mine, sh);
-  const bool by_k = t > 0.f && k >= 1 && k < a.vocab, short_k = by_k && k <= kList / 2, by_p = t > 0.f && !by_k && p < 1.f;
+  const bool by_k = t > 0.f && k >= 1 && k < a.vocab, short_k = by_k && k <= kList / 2, long_k = by_k && !short_k, by_p = t > 0.f && !by_k && p < 1.f;
   const float least = mp > 0.f ? top + __builtin_amdgcn_logf(mp) / rate : bottom;     // z >= max z + ln min_p, on logits
-  if (threadIdx.x == 0) sh.n_sure = sh.n_list = 0;
-  sh.list[threadIdx.x] = 0;
+  clear_lists(sh);
 
-  // what the second pass needs: the least candidate for top-k, empty bins for top-p
+  // what the second pass needs: the least candidate for a short top-k, empty bins for a long one and for top-p
   float lo = __builtin_inff();
   if (short_k) {
     sh.count[threadIdx.x] = 0;
@@ -383,12 +416,13 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     // a little below the bin's edge, so that rounding leaves none of its logits out; the last bin is open
     const u32 bin = sh.digit;
     lo = bin >= kBins - 1 || all < (u32)k ? -3.402823466e38f : top - ((float)(bin + 1) * 0.0625f / rate) * 1.00001f;
-  } else if (by_p) {
-#pragma unroll
-    for (int j = 0; j < kMassBins / kSampleThreads; ++j) sh.mass[j * kSampleThreads + threadIdx.x] = 0;
+  } else if (by_p || long_k) {
+    clear_bins(sh);
   }
   __syncthreads();
 
+  auto bin_at = [](float d) { return (u32)(int)(d * 128.f); };       // d in log2 below the largest, under 32
+  auto bin_of = [&](float v) { return bin_at(fminf((top - v) * rate, 31.995f)); };
   List list = {sh.list, &sh.n_list}, sure = {sh.sure, &sh.n_sure};
   float total = 0.f;
   u64 m = 0;
@@ -401,7 +435,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       bits |= v[i] >= lo ? 1u << i : 0u;
       if (by_p) {
         const u32 w = (u32)(e * kMassUnit);
-        if (w > 0) atomicAdd(&sh.mass[min((int)(d * 128.f), kMassBins - 1)], (u64)w);
+        if (w > 0) atomicAdd(&sh.mass[bin_at(d)], (u64)w);
         m += w;
       }
     }
@@ -423,8 +457,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   u64 best = 0;
   Cut cut = {key_of(bottom) + 1u, 0xffffffffu};
   u32 bin = 0xffffffffu;                  // top-p: the bin that the cut lies in
-  auto bin_of = [&](float v) { return (u32)min((int)((top - v) * rate * 128.f), kMassBins - 1); };
-  bool done = false;
+  bool done = false, general = false;     // general: one copy of that code
 
   if (t == 0.f) {
     x.batches([&](const float (&v)[16], auto &&index) {
@@ -453,33 +486,70 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     }
     if (stays && (v >= least || v == top)) best = score(me);
     done = true;
-  } else if (by_k) {
-    cut = general_cut<TYPE>(row, a.vocab, k, p, top, rate, sh);
-  } else if (by_p) {
+  } else if (short_k) {
+    general = true;
+  }
+  // what the cut so far leaves
+  float edge = bottom;
+  u32 edge_at = 0;
+  auto kept = [&](float v, u32 at) { return v > edge || (v == edge && v > bottom && at <= edge_at); };
+  bool search_p = by_p;
+  if (long_k) {
+    x.batches([&](const float (&v)[16], auto &&) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (v[i] > bottom) atomicAdd(&sh.mass[bin_of(v[i])], 1ull);
+    });
+    __syncthreads();
+    const u32 b = find_bin((double)k, sh);
+    search_p = p < 1.f;
+    if (b != 0xffffffffu) {               // else fewer than k finite logits
+      const u32 above = (u32)sh.total;
+      x.batches([&](const float (&v)[16], auto &&index) {
+        u32 bits = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bits |= v[i] > bottom && bin_of(v[i]) == b ? 1u << i : 0u;
+        list.add(x, bits, index);
+      });
+      __syncthreads();
+      const u32 n = sh.n_list;
+      if (n > (u32)kList) {
+        general = true;
+        search_p = false;
+      } else {
+        const u64 me = sh.list[threadIdx.x];
+        sh.count[threadIdx.x] = 0;
+        __syncthreads();
+        u32 rank;
+        u64 none;
+        precede(sh.list, sh.count, threadIdx.x < n ? n : 0u, me, &rank, &none);
+        if (threadIdx.x < n && above + rank + 1 == (u32)k) sh.cut = me;
+        __syncthreads();
+        cut = Cut{(u32)(sh.cut >> 32), entry_at(sh.cut)};
+        edge = logit_of(cut.key);
+        edge_at = cut.at;
+      }
+    }
+    if (search_p) {                       // masses of what stayed
+      clear_bins(sh);
+      clear_lists(sh);
+      __syncthreads();
+      x.batches([&](const float (&v)[16], auto &&index) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float d = (top - v[i]) * rate;
+          const u32 w = kept(v[i], (u32)index(i)) && d < 32.f ? (u32)(__builtin_amdgcn_exp2f(-d) * kMassUnit) : 0u;
+          if (w > 0) atomicAdd(&sh.mass[bin_at(d)], (u64)w);
+          m += w;
+        }
+      });
+    }
+  }
+  if (search_p) {
     // the bin in which the wanted mass is reached
     m = block_add(m, sh);
     const double want = fmax((double)p * (double)m, 1.0);
-    constexpr int kEach = kMassBins / kSampleThreads;
-    u64 own[kEach], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) sum += own[j] = sh.mass[threadIdx.x * kEach + j];
-    const u64 mine_all = sum;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    sum = wave_scan(sum, (u64)0, [](u64 a, u64 b) { return a + b; });
-    if (lane == 63) sh.wave_mass[wave] = sum;
-    __syncthreads();
-    u64 ahead = sum - mine_all;
-    for (int w = 0; w < wave; ++w) ahead += sh.wave_mass[w];
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      if ((double)ahead < want && (double)(ahead + own[j]) >= want) {
-        sh.digit = threadIdx.x * kEach + j;
-        sh.total = ahead;
-      }
-      ahead += own[j];
-    }
-    __syncthreads();
-    bin = sh.digit;
+    bin = find_bin(want, sh);
     const u64 above = sh.total;
     // its logits into one list, those before it into another: only what min_p leaves, which changes no order and no mass before
     x.batches([&](const float (&v)[16], auto &&index) {
@@ -487,7 +557,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const u32 b = bin_of(v[i]);
-        const bool on = v[i] > bottom && (v[i] >= least || v[i] == top);
+        const bool on = kept(v[i], (u32)index(i)) && (v[i] >= least || v[i] == top);
         inside |= on && b == bin ? 1u << i : 0u;
         before |= on && b < bin ? 1u << i : 0u;
       }
@@ -497,7 +567,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     __syncthreads();
     const u32 n = sh.n_list, n_sure = sh.n_sure;
     if (n > (u32)kList) {
-      cut = general_cut<TYPE>(row, a.vocab, 0, p, top, rate, sh);
+      general = true;
     } else {
       const bool on = threadIdx.x < n;
       const u64 me = sh.list[threadIdx.x];
@@ -525,16 +595,17 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       }
     }
   }
+  if (general) cut = general_cut<TYPE>(row, a.vocab, k, p, top, rate, sh);
   if (!done) {
     // many, or none left out: the random numbers of what stays by logit and, at the cut, by index.  Before the cut's bin
     // nothing is left out but by min_p.
     const bool binned = cut.key == 0xffffffffu;
-    const float edge = binned ? __builtin_inff() : logit_of(cut.key);
+    const float last = binned ? __builtin_inff() : logit_of(cut.key);
     x.batches([&](const float (&v)[16], auto &&index) {
       u32 bits = 0;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const bool in = binned ? bin_of(v[i]) < bin : v[i] > edge || (v[i] == edge && (u32)index(i) <= cut.at);
+        const bool in = binned ? bin_of(v[i]) < bin : v[i] > last || (v[i] == last && (u32)index(i) <= cut.at);
         bits |= v[i] > bottom && in && (v[i] >= least || v[i] == top) ? 1u << i : 0u;
       }
       if (bits == 0) return;

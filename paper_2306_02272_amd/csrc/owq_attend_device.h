@@ -145,17 +145,20 @@ __device__ __forceinline__ h8_t weights(const f32x4 (&s)[2], const Tile<STEPS> &
     most = fmaxf(most, pv[i]);
   }
   if (__any(most > kLimit)) {
-    float y[8], top = -__builtin_inff();
+    float top = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const u32 km = t.km[i >> 2][i & 3], vm = t.vm[i >> 2][i & 3];
-      y[i] = __builtin_fmaf(half_lo(km), s[i >> 2][i & 3] * w.c1[n], half_hi(km) * w.x1[n]);
-      const float z = fmaxf(top, y[i] + __builtin_amdgcn_logf(half_lo(vm)));
+      const float y = __builtin_fmaf(half_lo(km), s[i >> 2][i & 3] * w.c1[n], half_hi(km) * w.x1[n]);
+      const float z = fmaxf(top, y + __builtin_amdgcn_logf(half_lo(vm)));
       top = on[i] ? z : top;
     }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float ref = fmaxf(w.ref[n], top - kRoom);
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    // rows that need it only: what other rows of the wave hold must not show in a row's rounding
+    const float ref = most > kLimit ? fmaxf(w.ref[n], top - kRoom) : w.ref[n];
     const float alpha = __builtin_amdgcn_exp2f(w.ref[n] - ref);
     w.ref[n] = ref;
     w.l[n] *= alpha;
@@ -165,7 +168,9 @@ __device__ __forceinline__ h8_t weights(const f32x4 (&s)[2], const Tile<STEPS> &
     w.mid[n] *= alpha;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      p[i] = __builtin_amdgcn_exp2f(y[i] - ref);
+      const u32 km = t.km[i >> 2][i & 3];          // as above, bit for bit
+      const float y = __builtin_fmaf(half_lo(km), s[i >> 2][i & 3] * w.c1[n], __builtin_fmaf(half_hi(km), w.x1[n], -ref));
+      p[i] = __builtin_amdgcn_exp2f(y);
       pv[i] = p[i] * half_lo(t.vm[i >> 2][i & 3]);
       if (EDGE) {
         p[i] = on[i] ? p[i] : 0.f;

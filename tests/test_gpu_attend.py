@@ -169,6 +169,25 @@ def test_what_is_masked_has_no_effect(env, new):
     assert torch.equal(got2[2:][clean[2:]], got[2:][clean[2:]])
 
 
+@pytest.mark.parametrize("new", [1, 5, 13, 90])
+def test_rows_do_not_show_in_each_other(env, new):
+    # sharp and NaN rows move their own reference, at other tiles than their neighbours: these keep every bit
+    torch, B = env
+    rng = np.random.default_rng(10)
+    pages, table = filled(env, rng, [700], 1, 64, 32)
+    args = (pages, i32(torch, table), i32(torch, [0, new]), i32(torch, [700]))
+    q = torch.from_numpy(rng.normal(size=(new, 4, 64))).half().cuda()
+    base = B.cache_attention(q, *args)
+    for factor in (300.0, -300.0, 0.0, float("nan")):
+        q2 = q.clone()
+        q2[:, 1] *= factor
+        q2[::3, 2] *= factor
+        got = B.cache_attention(q2, *args)
+        same = torch.ones(new, 4, dtype=torch.bool, device="cuda")
+        same[:, 1], same[::3, 2] = False, False
+        assert torch.equal(got[same], base[same]), factor
+
+
 def test_no_page_is_no_key(env):
     torch, B = env
     rng = np.random.default_rng(8)

@@ -1,5 +1,5 @@
-// Attention over the 4-bit cache, few rows per sequence and key/value head (64 or fewer): single tokens, drafts, short
-// pieces.  The keys are what there is to read.  Every (sequence, head) has its tiles cut into ranges of equal length, one
+// Attention over the 4-bit cache, few rows: single tokens, drafts, short pieces.  The keys are what there is to read.  Every
+// (sequence, head, block of 16 or 32 rows) has its tiles cut into ranges of equal length, one
 // workgroup each; how long a range is at most goes by the sum of all sequences' tiles, so that the workgroups are as many
 // as the compute units hold at once, whatever the lengths.  A workgroup finds its range by sums over the sequences.  Its
 // waves take every fourth tile and are joined in LDS; ranges are joined by a second launch.
@@ -37,7 +37,7 @@ __device__ __forceinline__ u64 sum_over(const AttendArgs &a, int mine, int lane,
 // Most tiles of a range: a.ranges of them over all heads, or as many more as it takes that every head has one.  Two
 // corrections bring their number to a.ranges or below where that can be.
 __device__ __forceinline__ int range_length(const AttendArgs &a, int mine, int lane) {
-  const u64 want = (u64)a.ranges, heads = (u64)a.c.kv_heads;
+  const u64 want = (u64)a.ranges, heads = (u64)a.c.kv_heads * a.blocks;
   const u64 total = sum_over(a, mine, lane, [](int n) { return (u64)n; }) * heads;
   u64 length = (total + want - 1) / want;
   length = length > (u64)a.least_tiles ? length : (u64)a.least_tiles;
@@ -69,7 +69,7 @@ __device__ __forceinline__ void store_row(const AttendArgs &a, const Sequence &s
 }
 
 template <int STEPS, int NQ>
-__global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
   constexpr int P = 32 * STEPS;
   __shared__ float red[kWaves][16][P + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident)
         tiles = tiles_of(a, mine);
       }
       const int own = tiles > 0 ? (tiles - 1) / length + 1 : 0;
-      const u64 cost = (u64)own * a.c.kv_heads;
+      const u64 cost = (u64)own * a.c.kv_heads * a.blocks;
       const u64 scan = wave_scan(cost, (u64)0, add64), from = before + scan - cost;
       const u64 here = __ballot(from <= blockIdx.x && blockIdx.x < from + cost);
       if (here != 0) {
@@ -111,12 +111,15 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident)
     a.places[2 * b] = (int)blockIdx.x;
     a.places[2 * b + 1] = ranges;
   }
-  const int head = place / ranges, range = place - head * ranges;
-  const int pa = sq.p0, pb = sq.p0 + (sq.n_rows - 1) / a.group;
+  const int item = place / ranges, range = place - item * ranges;
+  const int head = item / a.blocks, first = (item - head * a.blocks) * 16 * NQ;
+  if (first >= sq.n_rows) return;
+  const int last = (first + 16 * NQ < sq.n_rows ? first + 16 * NQ : sq.n_rows) - 1;
+  const int pa = sq.p0 + first / a.group, pb = sq.p0 + last / a.group;
   const Span span = visible_tiles(a, pa, pb);
   const int i0 = (int)((int64_t)span.count * range / ranges), i1 = (int)((int64_t)span.count * (range + 1) / ranges);
   Rows<STEPS, NQ> w;
-  attend_span<kWaves>(a, sq, span, b, head, 0, pa, pb, i0, i1, wave, lane, w);
+  attend_span<kWaves>(a, sq, span, b, head, first, pa, pb, i0, i1, wave, lane, w);
 
   // the waves joined: column sums of a row lie in the lanes of its column
 #pragma unroll
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident)
     }
     __syncthreads();
     const int r = threadIdx.x >> 4, part = threadIdx.x & 15;      // row, columns part * 2 STEPS and on
-    const int row = 16 * n + r;
+    const int row = first + 16 * n + r;
     if (row < sq.n_rows) {
       float ref = red[0][r][P];
 #pragma unroll
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ >= 4 ? 1 : NQ == 2 ? 2 : kResident)
       if (ranges == 1) {
         store_row<STEPS>(a, sq, head, row, part, o, ref, total);
       } else {
-        const int64_t slot = (int64_t)blockIdx.x * a.slot_rows + row;
+        const int64_t slot = (int64_t)blockIdx.x * a.slot_rows + 16 * n + r;
         float *dst = a.part + slot * P + part * 2 * STEPS;
 #pragma unroll
         for (int e = 0; e < 2 * STEPS; ++e) dst[e] = o[e];
@@ -176,7 +179,8 @@ __global__ __launch_bounds__(64 * kWaves) void owq_attend_join_kernel(AttendArgs
   if (row >= sq.n_rows) return;
   const int used = a.places[2 * b + 1];
   if (used == 1) return;
-  const int64_t slot0 = (int64_t)(a.places[2 * b] + head * used) * a.slot_rows + row;
+  const int block = row / a.slot_rows;
+  const int64_t slot0 = (int64_t)(a.places[2 * b] + (head * a.blocks + block) * used) * a.slot_rows + row - block * a.slot_rows;
   auto slot_of = [&](int s) { return slot0 + (int64_t)s * a.slot_rows; };
   float ref = kNoRef;
   for (int s = lane; s < used; s += 64) ref = fmaxf(ref, a.part_sums[2 * slot_of(s)]);
@@ -208,25 +212,34 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   AttendPlan p{};
   p.group = a.q_heads / d.kv_heads;
   const int64_t rows = (int64_t)a.max_new * p.group;
-  p.many = rows > 64;
-  if (p.many) return p;
-  // 64 rows or fewer: 16, 32 or 64 of them per wave
-  p.col_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   int64_t seen = std::min<int64_t>(a.max_len, (int64_t)d.table_stride * d.page_size);
   if (a.window > 0) seen = std::min<int64_t>(seen, (int64_t)a.window + a.max_new + a.sinks + 96);
   const int64_t tiles = std::max<int64_t>(1, (seen + 31) / 32);
-  const int64_t items = (int64_t)d.n_seqs * d.kv_heads;
-  // as many workgroups as the compute units hold at once (of four waves, by registers), two tiles per wave at least;
-  // where no sequence has more than four tiles per wave, whole items and no joining
-  const int64_t resident = 256 * (p.col_tiles == 4 ? 1 : p.col_tiles == 2 ? 2 : kResident);
+  const int64_t heads = (int64_t)d.n_seqs * d.kv_heads;
+  // Rows in blocks of 128 by whole spans read the keys least often; in blocks of 16 or 32 with the keys cut into ranges they
+  // fill the machine with few of them.  Where the blocks of 128 are a workgroup per compute unit, the first is as fast or
+  // faster (1 x 1000 of 1000 tokens, 32/8 heads, 256 blocks: 36 us, 43 with ranges); below that it is slower (300 of 2000,
+  // 32/32 heads, 96 blocks: 67 us, 39 with ranges; 600 of 4000, 152 blocks: 125 us, 104), but for short spans of half a
+  // machine's blocks, where a launch to join costs more (3 x 300 of 300, 204 blocks: 18 us, 26 with ranges).
+  const int64_t wide = heads * ((rows + 127) / 128);
+  p.many = rows > 64 && (wide >= 256 || (wide >= 128 && tiles <= 16));
+  if (p.many) return p;
+  p.col_tiles = rows <= 16 ? 1 : 2;
+  p.rows = (int)rows;
+  p.slot_rows = (int)std::min<int64_t>(rows, 16 * p.col_tiles);
+  p.blocks = (int)((rows + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
+  const int64_t items = heads * p.blocks;
+  // As many workgroups as the compute units hold at once, two tiles per wave at least; where no sequence has more than four
+  // tiles per wave, or the heads are many and the spans short, whole spans and no second launch (512 heads on spans of 36
+  // tiles: 15.9 us, 20.8 with ranges).
+  const int64_t resident = 256 * (p.col_tiles == 2 ? 2 : kResident);
   p.whole = tiles <= 4 * 4 || (items >= 256 && tiles <= 16 * 4);
   p.least_tiles = 2 * 4;
-  // heads that fill the compute units by themselves come in turns, and twice the ranges even out their lengths
+  // items that fill the compute units by themselves come in turns, and twice the ranges even out their lengths
   p.ranges = (int)(2 * items <= resident ? resident : 2 * resident);
-  // no more workgroups than p.ranges ranges and one more per head; nor than ranges of the least length
+  // no more workgroups than p.ranges ranges and one more per item; nor than ranges of the least length
   p.workgroups = (int)(p.whole ? items : std::min(p.ranges + items, items * ((tiles + p.least_tiles - 1) / p.least_tiles)));
-  p.rows = (int)rows;
-  p.slots = p.whole ? 0 : (size_t)p.workgroups * rows;
+  p.slots = p.whole ? 0 : (size_t)p.workgroups * p.slot_rows;
   const int P = (d.head_dim + 31) / 32 * 32;
   p.workspace = p.whole ? 0 : p.slots * (P + 2) * 4 + (size_t)d.n_seqs * 8;
   return p;
@@ -244,8 +257,7 @@ template <int STEPS>
 static void launch_steps(const AttendArgs &a, const AttendPlan &p, hipStream_t s) {
   if (p.many) launch_attend_many<STEPS>(a, s);
   else if (p.col_tiles == 1) launch_few<STEPS, 1>(a, p, s);
-  else if (p.col_tiles == 2) launch_few<STEPS, 2>(a, p, s);
-  else launch_few<STEPS, 4>(a, p, s);
+  else launch_few<STEPS, 2>(a, p, s);
 }
 
 int launch_attend(const CacheView &c, const owq_attention_desc_t &d, const AttendPlan &p, const void *q, void *out, float *lse,
@@ -262,7 +274,7 @@ int launch_attend(const CacheView &c, const owq_attention_desc_t &d, const Atten
   a.q_heads = d.q_heads, a.group = p.group, a.max_new = d.max_new, a.window = d.window, a.sinks = d.sinks, a.max_len = d.max_len;
   a.bf16 = d.type == OWQ_TYPE_BF16;
   a.places = reinterpret_cast<int32_t *>(a.part_sums + 2 * p.slots);
-  a.slot_rows = p.rows, a.least_tiles = p.least_tiles, a.ranges = p.ranges, a.whole = p.whole;
+  a.slot_rows = p.slot_rows, a.blocks = p.blocks, a.least_tiles = p.least_tiles, a.ranges = p.ranges, a.whole = p.whole;
   a.scale = d.scale * 1.44269504089f;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   switch (steps) {

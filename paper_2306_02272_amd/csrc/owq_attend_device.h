@@ -45,7 +45,7 @@ struct AttendArgs {
   int64_t q_row, q_head;
   int32_t q_heads, group, max_new, window, sinks, max_len, bf16;
   int32_t *places;       // few rows: [sequence][2], its first workgroup and its ranges per head
-  int32_t slot_rows, least_tiles, ranges, whole;
+  int32_t slot_rows, blocks, least_tiles, ranges, whole;
   float scale;           // log2 e included
 };
 

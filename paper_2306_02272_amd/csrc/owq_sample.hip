@@ -9,7 +9,10 @@
 //     the bin in which the wanted sum is reached are listed and ranked in the same way.  Three passes for either.
 // A bin with more than 1024 logits, as in flat rows, takes the general way: keys by four histograms of eight bits each.  Passes are rolled loops of 16 logits per thread: with the row in registers every pass is
 // straight-line code that a launch runs through once, and its instructions come from memory more slowly than the row does
-// (179 us for 256 rows of 50 272 fp32 logits so).
+// (179 us for 256 rows of 50 272 fp32 logits so, 36 now).
+//
+// Bound by the passes: those 256 rows with top-p take three, the first from memory, the others from the last-level cache:
+// 36.3 us for 103 MB of logits and variates; one row of 50 272 11.0 us, 10.5 of them in the kernel.
 // Masses are 2^31 e^(z - max z) as integers, so that no order of additions shows.
 #include <hip/hip_runtime.h>
 

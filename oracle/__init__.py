@@ -29,6 +29,8 @@ Pins (see tests marked "not gpu"):
   owq_backward_ref (derivatives for weak-column tuning) the adjoint identities against the pinned
                    forward oracle, unit-vector responses entry by entry, central differences
                    of the forward loops, all columns weak, nested loops.
+  step             (what lies between two layers) rotations by quarter turns, gradients against differences, codes and words
+                   of a tile by hand, attention over equal scores, sampling frequencies.
   Numerics of y on the paper's real checkpoints: parity unpinned (the paper
   prints no output values and ships no weights).
 """

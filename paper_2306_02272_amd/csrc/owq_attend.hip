@@ -2,7 +2,7 @@
 // (sequence, head, block of 16 or 32 rows) has its tiles cut into ranges of equal length, one
 // workgroup each; how long a range is at most goes by the sum of all sequences' tiles, so that the workgroups are as many
 // as the compute units hold at once, whatever the lengths.  A workgroup finds its range by sums over the sequences.  Its
-// waves take every fourth tile and are joined in LDS; ranges are joined by a second launch.
+// waves take tiles in turn and are joined in LDS; ranges are joined by a second launch.
 //
 // Bound by memory where there is enough of it: one token each of 64 sequences of 300 to 8192, 32/8 heads of 128, in 76.6 us, 298 MB
 // at 3.9 TB/s.  One token of 40/40 heads behind 4000 takes 17.3 us, 4 of them in the second launch: latency of what a
@@ -73,10 +73,10 @@ __device__ __forceinline__ void store_row(const AttendArgs &a, const Sequence &s
   if (a.lse != nullptr && part == 0) a.lse[at * a.q_heads + h] = lse_of(ref, total);
 }
 
-template <int STEPS, int NQ, bool SPLIT>
-__global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
+template <int STEPS, int NQ, bool SPLIT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, NQ == 2 || WAVES == 8 ? 2 : kResident) void owq_attend_few_kernel(AttendArgs a) {
   constexpr int P = 32 * STEPS;
-  __shared__ float red[kWaves][16][P + 4];
+  __shared__ float red[WAVES][16][P + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int quad = lane >> 4, col = lane & 15;
 
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_atte
   const Span span = visible_tiles(a, pa, pb);
   const int i0 = (int)((int64_t)span.count * range / ranges), i1 = (int)((int64_t)span.count * (range + 1) / ranges);
   Rows<STEPS, NQ> w;
-  attend_span<SPLIT, kWaves>(a, sq, span, b, head, first, pa, pb, i0, i1, wave, lane, w);
+  attend_span<SPLIT, WAVES>(a, sq, span, b, head, first, pa, pb, i0, i1, wave, lane, w);
 
   // the waves joined: column sums of a row lie in the lanes of its column
 #pragma unroll
@@ -145,15 +145,15 @@ __global__ __launch_bounds__(64 * kWaves, NQ == 2 ? 2 : kResident) void owq_atte
     __syncthreads();
     const int r = threadIdx.x >> 4, part = threadIdx.x & 15;      // row, columns part * 2 STEPS and on
     const int row = first + 16 * n + r;
-    if (row < sq.n_rows) {
+    if (r < 16 && row < sq.n_rows) {
       float ref = red[0][r][P];
 #pragma unroll
-      for (int v = 1; v < kWaves; ++v) ref = fmaxf(ref, red[v][r][P]);
+      for (int v = 1; v < WAVES; ++v) ref = fmaxf(ref, red[v][r][P]);
       float total = 0.f, o[2 * STEPS];
 #pragma unroll
       for (int e = 0; e < 2 * STEPS; ++e) o[e] = 0.f;
 #pragma unroll
-      for (int v = 0; v < kWaves; ++v) {
+      for (int v = 0; v < WAVES; ++v) {
         const float f = __builtin_amdgcn_exp2f(red[v][r][P] - ref);
         total = __builtin_fmaf(f, red[v][r][P + 1], total);
 #pragma unroll
@@ -234,14 +234,19 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   p.slot_rows = (int)std::min<int64_t>(rows, 16 * p.col_tiles);
   p.blocks = (int)((rows + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
   const int64_t items = heads * p.blocks;
-  // As many workgroups as the compute units hold at once, two tiles per wave at least; where no sequence has more than four
-  // tiles per wave, or the heads are many and the spans short, whole spans and no second launch (512 heads on spans of 36
-  // tiles: 16.5 us, 26 with ranges).
+  // As many workgroups as the compute units hold at once, two tiles per wave at least; whole spans and no second launch where
+  // no sequence has more than four tiles per wave, or where the heads are many and the spans short (512 heads on spans of 36
+  // tiles, 8 waves: 14.5 us, 26 with ranges of 4 waves).  Whole spans of more than 16
+  // tiles have 8 waves where the compute units take all workgroups at once, one of them each with 68 KB of LDS, two up to
+  // 64 columns (256 heads of 128 columns on spans of up to 47 tiles: 15.9 us, 19.4 with 4 waves; 512 on 19 tiles: 20 us, 16 with 4).
   const int64_t resident = 256 * (p.col_tiles == 2 ? 2 : kResident);
-  p.whole = tiles <= 4 * 4 || (items >= 256 && tiles <= 16 * 4);
-  p.least_tiles = 2 * 4;
-  // items that fill the compute units by themselves come in turns, and twice the ranges even out their lengths
-  p.ranges = (int)(2 * items <= resident ? resident : 2 * resident);
+  p.waves = p.col_tiles == 1 && tiles > 16 && items <= (d.head_dim <= 64 ? 512 : 256) ? 8 : 4;
+  p.whole = tiles <= 4 * p.waves || (items >= 256 && tiles <= 64);
+  if (!p.whole) p.waves = 4;
+  p.least_tiles = 2 * p.waves;
+  // Items that fill the compute units by themselves come in turns, and twice the ranges even out their lengths.  More than 32
+  // ranges of an item cost more to join than they gain (30 000 tokens of 32/8 heads: 21.3 us, 26.1 with 96).
+  p.ranges = (int)(2 * items <= resident ? std::min(resident, 32 * items) : 2 * resident);
   // no more workgroups than p.ranges ranges and one more per item; nor than ranges of the least length
   p.workgroups = (int)(p.whole ? items : std::min(p.ranges + items, items * ((tiles + p.least_tiles - 1) / p.least_tiles)));
   p.slots = p.whole ? 0 : (size_t)p.workgroups * p.slot_rows;
@@ -250,10 +255,10 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   return p;
 }
 
-template <int STEPS, int NQ>
+template <int STEPS, int NQ, int WAVES>
 static void launch_few(const AttendArgs &a, const AttendPlan &p, hipStream_t s) {
-  if (a.bf16) owq_attend_few_kernel<STEPS, NQ, false><<<p.workgroups, 64 * kWaves, 0, s>>>(a);
-  else owq_attend_few_kernel<STEPS, NQ, true><<<p.workgroups, 64 * kWaves, 0, s>>>(a);
+  if (a.bf16) owq_attend_few_kernel<STEPS, NQ, false, WAVES><<<p.workgroups, 64 * WAVES, 0, s>>>(a);
+  else owq_attend_few_kernel<STEPS, NQ, true, WAVES><<<p.workgroups, 64 * WAVES, 0, s>>>(a);
   if (!p.whole)
     owq_attend_join_kernel<<<dim3((unsigned)((p.rows + kWaves - 1) / kWaves), (unsigned)a.c.kv_heads, (unsigned)a.c.n_seqs), 64 * kWaves, 0, s>>>(
         a, 32 * STEPS);
@@ -262,8 +267,9 @@ static void launch_few(const AttendArgs &a, const AttendPlan &p, hipStream_t s) 
 template <int STEPS>
 static void launch_steps(const AttendArgs &a, const AttendPlan &p, hipStream_t s) {
   if (p.many) launch_attend_many<STEPS>(a, s);
-  else if (p.col_tiles == 1) launch_few<STEPS, 1>(a, p, s);
-  else launch_few<STEPS, 2>(a, p, s);
+  else if (p.col_tiles == 2) launch_few<STEPS, 2, 4>(a, p, s);
+  else if (p.waves == 8) launch_few<STEPS, 1, 8>(a, p, s);
+  else launch_few<STEPS, 1, 4>(a, p, s);
 }
 
 int launch_attend(const CacheView &c, const owq_attention_desc_t &d, const AttendPlan &p, const void *q, void *out, float *lse,

@@ -45,6 +45,7 @@ struct AttendPlan {
   bool many;            // whole spans of keys for 128 rows; else ranges of them for 16 or 32, and:
   int32_t rows;         // most rows (new tokens x group) of a sequence and key/value head
   int32_t col_tiles;    // 16-row tiles of a wave
+  int32_t waves;        // of a workgroup
   int32_t blocks, slot_rows;   // blocks of so many rows
   bool whole;           // one workgroup per sequence, head and block
   int32_t ranges, least_tiles, workgroups;

@@ -87,3 +87,21 @@ def test_masked_keys_missing_pages_and_spoilt_rows(env):      # noqa: F811
         B.cache_append(pages, i32(torch, table), i32(torch, [0, 1]), i32(torch, [t + 1]), bad, bad)
     got = B.cache_attention(q, *args, window=100, sinks=3)
     assert torch.equal(got[:-1], base[:-1]) and torch.isnan(got[-1]).all()
+
+
+@pytest.mark.parametrize("case", [  # one token each: heads and spans that take eight waves, four, ranges
+    ([350], 8, 2, 128, 0, 0, False), ([1000, 300], 40, 20, 64, 0, 0, True), ([1500, 290, 900, 64] * 4, 32, 16, 32, 0, 0, False),
+    ([900, 2000] * 4, 64, 32, 32, 500, 3, False), ([700, 33] * 9, 32, 32, 24, 0, 0, True), ([9000], 2, 1, 96, 0, 0, False),
+], ids=lambda c: "%d to %d, %d heads" % (len(c[0]), max(c[0]), c[2]))
+def test_single_tokens(env, case):      # noqa: F811
+    torch, B = env
+    lengths, hq, hk, dim, window, sinks, bf16 = case
+    rng = np.random.default_rng(sum(lengths) + hq)
+    pages, table = filled(env, rng, lengths, hk, dim, 64)
+    n = len(lengths)
+    q = torch.from_numpy(rng.normal(size=(n, hq, dim)) * 1.5).to(torch.bfloat16 if bf16 else torch.float16).cuda()
+    starts = np.arange(n + 1)
+    out, lse = B.cache_attention(q, pages, i32(torch, table), i32(torch, starts), i32(torch, lengths), window=window, sinks=sinks,
+                                 max_new=1, max_len=max(lengths), want_lse=True)
+    want = step.attention(q.double().cpu().numpy(), pages.cpu().numpy(), table, starts, lengths, dim ** -0.5, window, sinks)
+    check(env, out, lse, want, bf16)

@@ -235,10 +235,10 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   p.blocks = (int)((rows + 16 * p.col_tiles - 1) / (16 * p.col_tiles));
   const int64_t items = heads * p.blocks;
   // As many workgroups as the compute units hold at once, two tiles per wave at least; whole spans and no second launch where
-  // no sequence has more than four tiles per wave, or where the heads are many and the spans short (512 heads on spans of 36
-  // tiles, 8 waves: 14.5 us, 26 with ranges of 4 waves).  Whole spans of more than 16
-  // tiles have 8 waves where the compute units take all workgroups at once, one of them each with 68 KB of LDS, two up to
-  // 64 columns (256 heads of 128 columns on spans of up to 47 tiles: 15.9 us, 19.4 with 4 waves; 512 on 19 tiles: 20 us, 16 with 4).
+  // no sequence has more than four tiles per wave, or where the heads are many and the spans short (512 heads of 64 columns on
+  // spans of 36 tiles, 8 waves: 14.5 us, 26 with ranges of 4 waves).  Whole spans of more than 16 tiles have 8 waves where the
+  // compute units take all workgroups at once, one each with 68 KB of LDS, two up to 64 columns (256 heads of 128 columns on
+  // spans of up to 47 tiles: 16 us, 19.3 with 4 waves; 512 heads on 19 tiles: 20 us, 16 with 4).
   const int64_t resident = 256 * (p.col_tiles == 2 ? 2 : kResident);
   p.waves = p.col_tiles == 1 && tiles > 16 && items <= (d.head_dim <= 64 ? 512 : 256) ? 8 : 4;
   p.whole = tiles <= 4 * p.waves || (items >= 256 && tiles <= 64);

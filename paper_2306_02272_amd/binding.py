@@ -467,7 +467,8 @@ def _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq=None, dk=
     (qt, qh, q1), (kt, kh, k1) = q.stride(), k.stride()
     n_positions, half = cos.shape
     f32 = torch.float32
-    assert q.is_cuda and k.is_cuda and k_tokens == tokens and k_dim == dim and k.dtype is q.dtype and q1 == 1 and k1 == 1, (q.shape, k.shape)
+    assert q.is_cuda and k.is_cuda and k_tokens == tokens and k_dim == dim and k.dtype is q.dtype, (q.shape, k.shape)
+    assert (q1 == 1 and k1 == 1) or tokens == 0, (q.stride(), k.stride())      # without elements strides mean nothing
     assert cos.dtype is f32 and sin.dtype is f32 and cos.is_cuda and sin.is_cuda and cos.is_contiguous() and sin.is_contiguous()
     assert cos.shape == sin.shape
     for w in (wq, wk):
@@ -475,7 +476,7 @@ def _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq=None, dk=
     dqt = dqh = dkt = dkh = 0
     if dq is not None:
         for d, x in ((dq, q), (dk, k)):
-            assert d.is_cuda and d.shape == x.shape and d.dtype is x.dtype and d.stride(2) == 1
+            assert d.is_cuda and d.shape == x.shape and d.dtype is x.dtype and (d.stride(2) == 1 or d.numel() == 0)
         dqt, dqh, dkt, dkh = dq.stride(0), dq.stride(1), dk.stride(0), dk.stride(1)
     return _ROPE.pack(tokens, q_heads, kv_heads, dim, 2 * half, interleaved, _type_of(q), n_positions, eps, 0, qt, qh, kt, kh, dqt, dqh, dkt,
                       dkh), tokens
@@ -545,7 +546,7 @@ def cache_append(pages, page_table, starts, lengths, k, v, max_new=None):
     torch = _torch()
     rows, heads, dim = k.shape
     (kr, kh, k1), (vr, vh, v1) = k.stride(), v.stride()
-    assert k.is_cuda and v.is_cuda and v.shape == k.shape and v.dtype is k.dtype and k1 == 1 and v1 == 1, (k.shape, v.shape)
+    assert k.is_cuda and v.is_cuda and v.shape == k.shape and v.dtype is k.dtype and ((k1 == 1 and v1 == 1) or rows == 0), (k.shape, v.shape)
     n_seqs = lengths.numel()
     desc, _ = _cache_args(pages, page_table, n_seqs, heads, dim)
     status = lib().owq_cache_append(desc, pages.data_ptr(), _int32(page_table, n_seqs, "page_table"), _int32(starts, n_seqs + 1, "starts"),
@@ -580,7 +581,7 @@ def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0,
     torch = _torch()
     rows, q_heads, dim = q.shape
     q_row, q_head, q1 = q.stride()
-    assert q.is_cuda and q1 == 1, q.shape
+    assert q.is_cuda and (q1 == 1 or rows == 0), q.shape
     n_seqs = lengths.numel()
     desc, most = _cache_args(pages, page_table, n_seqs, pages.shape[1], dim)
     if out is None:
@@ -615,11 +616,11 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
     rows, vocab = logits.shape
     row, one = logits.stride()
     f32 = torch.float32
-    assert logits.is_cuda and (one == 1 or vocab == 1), logits.stride()
+    assert logits.is_cuda and (one == 1 or vocab == 1 or rows == 0), logits.stride()
     noise_row = 0
     if noise is not None:
         noise_row, one = noise.stride()
-        assert noise.is_cuda and noise.dtype is f32 and noise.shape == logits.shape and (one == 1 or vocab == 1), noise.shape
+        assert noise.is_cuda and noise.dtype is f32 and noise.shape == logits.shape and (one == 1 or vocab == 1 or rows == 0), noise.shape
     for x in (temperature, top_p, min_p):
         assert x is None or (x.is_cuda and x.dtype is f32 and x.is_contiguous() and x.numel() == rows)
     token, logprob = logits.new_empty(rows, dtype=torch.int32), logits.new_empty(rows, dtype=f32)

@@ -56,12 +56,13 @@ owq_status_t owq_qk_norm_rope_backward(const owq_rope_desc_t *d, const void *dq_
   if (d->n_tokens > 0) {
     if (!dq_out || !dq || !cos || !sin || !positions || (wq && !q)) return OWQ_ERR_NULL;
     if (d->kv_heads > 0 && (!dk_out || !dk || (wk && !k))) return OWQ_ERR_NULL;
+    if (!rows16(dq_out, d->dq_token, d->dq_head) || !aligned(dq, 16)) return OWQ_ERR_BUFFER;
+    if (wq && !rows16(q, d->q_token, d->q_head)) return OWQ_ERR_BUFFER;
+    if (d->kv_heads > 0 && (!rows16(dk_out, d->dk_token, d->dk_head) || !aligned(dk, 16))) return OWQ_ERR_BUFFER;
+    if (wk && !rows16(k, d->k_token, d->k_head)) return OWQ_ERR_BUFFER;
+    if (!aligned(cos, 4) || !aligned(sin, 4) || !aligned(positions, 4)) return OWQ_ERR_BUFFER;
   }
-  if (!rows16(dq_out, d->dq_token, d->dq_head) || !aligned(dq, 16) || !aligned(wq, 16) || !aligned(wk, 16)) return OWQ_ERR_BUFFER;
-  if (wq && !rows16(q, d->q_token, d->q_head)) return OWQ_ERR_BUFFER;
-  if (d->kv_heads > 0 && (!rows16(dk_out, d->dk_token, d->dk_head) || !aligned(dk, 16))) return OWQ_ERR_BUFFER;
-  if (wk && !rows16(k, d->k_token, d->k_head)) return OWQ_ERR_BUFFER;
-  if (!aligned(cos, 4) || !aligned(sin, 4) || !aligned(positions, 4) || !aligned(dwq, 4) || !aligned(dwk, 4)) return OWQ_ERR_BUFFER;
+  if (!aligned(wq, 16) || !aligned(wk, 16) || !aligned(dwq, 4) || !aligned(dwk, 4)) return OWQ_ERR_BUFFER;
   RopePtrs p{};
   p.q = q, p.k = k, p.wq = wq, p.wk = wk, p.cos = cos, p.sin = sin, p.positions = positions;
   p.dq_out = dq_out, p.dk_out = dk_out, p.q_out = dq, p.k_out = dk, p.dwq = dwq, p.dwk = dwk;

@@ -406,7 +406,7 @@ owq_status_t owq_linear_backward(owq_handle_t h, const void *dy, const void *x, 
  *     dw = sum g x r,   dx = r (h - x r^2 mean(h x))          (dx = g without a weight)
  * workspace: owq_qk_norm_rope_backward_workspace_bytes bytes, 16-byte aligned, contents
  * undefined before and after (may be NULL if it is 0 bytes or no weight's gradient is wanted).  Without
- * tokens the weights' gradients are 0.
+ * tokens the weights' gradients are 0, without key heads that of wk is.
  */
 typedef struct {
   int32_t n_tokens, q_heads, kv_heads, head_dim, rotary_dim;

@@ -50,7 +50,6 @@ owq_status_t owq_qk_norm_rope_backward(const owq_rope_desc_t *d, const void *dq_
                                        void *workspace, size_t workspace_bytes, void *stream) {
   const owq_status_t st = check_rope(d);
   if (st != OWQ_OK) return st;
-  if (d->kv_heads == 0) wk = nullptr, dwk = nullptr;
   if (!wq) dwq = nullptr;
   if (!wk) dwk = nullptr;
   if (d->n_tokens > 0) {
@@ -59,7 +58,7 @@ owq_status_t owq_qk_norm_rope_backward(const owq_rope_desc_t *d, const void *dq_
     if (!rows16(dq_out, d->dq_token, d->dq_head) || !aligned(dq, 16)) return OWQ_ERR_BUFFER;
     if (wq && !rows16(q, d->q_token, d->q_head)) return OWQ_ERR_BUFFER;
     if (d->kv_heads > 0 && (!rows16(dk_out, d->dk_token, d->dk_head) || !aligned(dk, 16))) return OWQ_ERR_BUFFER;
-    if (wk && !rows16(k, d->k_token, d->k_head)) return OWQ_ERR_BUFFER;
+    if (d->kv_heads > 0 && wk && !rows16(k, d->k_token, d->k_head)) return OWQ_ERR_BUFFER;
     if (!aligned(cos, 4) || !aligned(sin, 4) || !aligned(positions, 4)) return OWQ_ERR_BUFFER;
   }
   if (!aligned(wq, 16) || !aligned(wk, 16) || !aligned(dwq, 4) || !aligned(dwk, 4)) return OWQ_ERR_BUFFER;

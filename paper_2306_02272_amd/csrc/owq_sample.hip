@@ -445,7 +445,9 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     if (short_k) list.add(x, bits, index);
   });
   total = block_sum(total, sh);           // NaN if a logit is (or the top infinite)
-  if (!(__builtin_fabsf(top) < __builtin_inff()) || total != total || !(t >= 0.f) || (t > 0.f && a.noise == nullptr)) {
+  // the temperature by itself: 1 / t of a subnormal one may still be finite, that of an infinite one is 0 and gives finite sums
+  const bool warm = t >= 0x1p-126f && t < __builtin_inff();
+  if (!(__builtin_fabsf(top) < __builtin_inff()) || total != total || !(t == 0.f || (warm && a.noise != nullptr))) {
     if (threadIdx.x == 0) {
       a.token[r] = -1;
       if (a.logprob) a.logprob[r] = __builtin_nanf("");

@@ -186,8 +186,9 @@ def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
     x = np.asarray(logits, np.float64)
     if np.isnan(x).any() or not np.isfinite(x.max()) or not 0 <= t < math.inf or 0 < t < 2.0 ** -126 or (t > 0 and noise is None):
         return -1, math.nan
-    z = x / (t if t > 0 else 1.0)
-    total = math.log(np.exp(z - z.max()).sum())          # beside the largest: it may be many times that
+    # beside the largest logit: at small temperatures the scaled logits themselves are so large that nothing can be added to them
+    z = (x - x.max()) / (t if t > 0 else 1.0)
+    total = math.log(np.exp(z).sum())
     order = np.argsort(-x, kind="stable")
     order = order[x[order] > -np.inf]
     token = order[0]
@@ -195,7 +196,7 @@ def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
         if 0 < top_k < len(order):
             order = order[:top_k]
         if top_p < 1:
-            p = np.exp(z[order] - z.max())
+            p = np.exp(z[order])
             keep = np.cumsum(p) - p < top_p * p.sum()
             keep[0] = True
             order = order[keep]
@@ -206,4 +207,4 @@ def sample_row(logits, noise, t=1.0, top_k=0, top_p=1.0, min_p=0.0):
         with np.errstate(divide="ignore"):
             score = z[order] - np.log(np.asarray(noise, np.float64)[order])
         token = order[score == score.max()].min()
-    return int(token), float(z[token] - z.max() - total)
+    return int(token), float(z[token] - total)

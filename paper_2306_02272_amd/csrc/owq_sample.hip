@@ -398,7 +398,11 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
   const float top = block_top(mine, sh);
   const bool by_k = t > 0.f && k >= 1 && k < a.vocab, short_k = by_k && k <= kList / 2, long_k = by_k && !short_k, by_p = t > 0.f && !by_k && p < 1.f;
-  const float least = mp > 0.f ? top + __builtin_amdgcn_logf(mp) / rate : bottom;     // z >= max z + ln min_p, on logits
+  // Everything is measured from the largest logit, in log2 of the probability: sums with a logit itself would round at its size,
+  // not at the difference's, and overflow at small temperatures.
+  auto below = [&](float v) { return (top - v) * rate; };
+  const float reach = mp > 0.f ? -__builtin_amdgcn_logf(mp) : __builtin_inff();       // z >= max z + ln min_p
+  auto likely = [&](float v) { return below(v) <= reach || v == top; };
   clear_lists(sh);
 
   // what the second pass needs: the least candidate for a short top-k, empty bins for a long one and for top-p
@@ -406,7 +410,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   if (short_k) {
     sh.count[threadIdx.x] = 0;
     __syncthreads();
-    const float d = (top - mine) * rate * 16.f;
+    const float d = below(mine) * 16.f;
     if (mine > bottom) atomicAdd(&sh.count[d < (float)(kBins - 1) ? (int)d : kBins - 1], 1u);
     __syncthreads();
     u32 all;
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   __syncthreads();
 
   auto bin_at = [](float d) { return (u32)(int)(d * 128.f); };       // d in log2 below the largest, under 32
-  auto bin_of = [&](float v) { return bin_at(fminf((top - v) * rate, 31.995f)); };
+  auto bin_of = [&](float v) { return bin_at(fminf(below(v), 31.995f)); };
   List list = {sh.list, &sh.n_list}, sure = {sh.sure, &sh.n_sure};
   float total = 0.f;
   u64 m = 0;
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     u32 bits = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float d = (top - v[i]) * rate, e = __builtin_amdgcn_exp2f(-d);
+      const float d = below(v[i]), e = __builtin_amdgcn_exp2f(-d);
       total += e;
       bits |= v[i] >= lo ? 1u << i : 0u;
       if (by_p) {
@@ -457,7 +461,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 
   const float *noise = a.noise + (int64_t)r * a.noise_row;
   auto score = [&](u64 e) {
-    return entry_of(__builtin_fmaf(entry_logit(e), rate, -__builtin_amdgcn_logf(noise[entry_at(e)])), entry_at(e));
+    return entry_of(__builtin_fmaf(entry_logit(e) - top, rate, -__builtin_amdgcn_logf(noise[entry_at(e)])), entry_at(e));
   };
   u64 best = 0;
   Cut cut = {key_of(bottom) + 1u, 0xffffffffu};
@@ -489,7 +493,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       const u64 mass = block_add(stays ? (u64)w : 0ull, sh);
       stays = stays && (double)ahead < fmax((double)p * (double)mass, 1.0);
     }
-    if (stays && (v >= least || v == top)) best = score(me);
+    if (stays && likely(v)) best = score(me);
     done = true;
   } else if (short_k) {
     general = true;
@@ -542,7 +546,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       x.batches([&](const float (&v)[16], auto &&index) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float d = (top - v[i]) * rate;
+          const float d = below(v[i]);
           const u32 w = kept(v[i], (u32)index(i)) && d < 32.f ? (u32)(__builtin_amdgcn_exp2f(-d) * kMassUnit) : 0u;
           if (w > 0) atomicAdd(&sh.mass[bin_at(d)], (u64)w);
           m += w;
@@ -562,7 +566,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const u32 b = bin_of(v[i]);
-        const bool on = kept(v[i], (u32)index(i)) && (v[i] >= least || v[i] == top);
+        const bool on = kept(v[i], (u32)index(i)) && likely(v[i]);
         inside |= on && b == bin ? 1u << i : 0u;
         before |= on && b < bin ? 1u << i : 0u;
       }
@@ -611,7 +615,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const bool in = binned ? bin_of(v[i]) < bin : v[i] > last || (v[i] == last && (u32)index(i) <= cut.at);
-        bits |= v[i] > bottom && in && (v[i] >= least || v[i] == top) ? 1u << i : 0u;
+        bits |= v[i] > bottom && in && likely(v[i]) ? 1u << i : 0u;
       }
       if (bits == 0) return;
       float u[16];
@@ -619,7 +623,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       for (int i = 0; i < 16; ++i) u[i] = noise[min(index(i), a.vocab - 1)];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const u64 o = entry_of(__builtin_fmaf(v[i], rate, -__builtin_amdgcn_logf(u[i])), (u32)index(i));
+        const u64 o = entry_of(__builtin_fmaf(v[i] - top, rate, -__builtin_amdgcn_logf(u[i])), (u32)index(i));
         best = ((bits >> i) & 1u) && o > best ? o : best;
       }
     });

@@ -82,6 +82,12 @@ __device__ __forceinline__ float block_sum(float v, SampleShared &sh) {
   return block_reduce(v, 0.f, sh.sum, [](float a, float b) { return a + b; });
 }
 
+// The instruction takes subnormal numbers for 0; scaled by 2^32 (exactly) they are normal.
+__device__ __forceinline__ float log2_of(float x) {
+  const bool small = x < 0x1p-126f;
+  return __builtin_amdgcn_logf(small ? x * 0x1p32f : x) - (small ? 32.f : 0.f);
+}
+
 __device__ __forceinline__ u32 mass_of(float x, float top, float rate) {
   return (u32)(__builtin_amdgcn_exp2f((x - top) * rate) * kMassUnit);
 }
@@ -401,7 +407,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   // Everything is measured from the largest logit, in log2 of the probability: sums with a logit itself would round at its size,
   // not at the difference's, and overflow at small temperatures.
   auto below = [&](float v) { return (top - v) * rate; };
-  const float reach = mp > 0.f ? -__builtin_amdgcn_logf(mp) : __builtin_inff();       // z >= max z + ln min_p
+  const float reach = mp > 0.f ? -log2_of(mp) : __builtin_inff();       // z >= max z + ln min_p
   auto likely = [&](float v) { return below(v) <= reach || v == top; };
   clear_lists(sh);
 
@@ -461,7 +467,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 
   const float *noise = a.noise + (int64_t)r * a.noise_row;
   auto score = [&](u64 e) {
-    return entry_of(__builtin_fmaf(entry_logit(e) - top, rate, -__builtin_amdgcn_logf(noise[entry_at(e)])), entry_at(e));
+    return entry_of(__builtin_fmaf(entry_logit(e) - top, rate, -log2_of(noise[entry_at(e)])), entry_at(e));
   };
   u64 best = 0;
   Cut cut = {key_of(bottom) + 1u, 0xffffffffu};
@@ -623,7 +629,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       for (int i = 0; i < 16; ++i) u[i] = noise[min(index(i), a.vocab - 1)];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const u64 o = entry_of(__builtin_fmaf(v[i] - top, rate, -__builtin_amdgcn_logf(u[i])), (u32)index(i));
+        const u64 o = entry_of(__builtin_fmaf(v[i] - top, rate, -log2_of(u[i])), (u32)index(i));
         best = ((bits >> i) & 1u) && o > best ? o : best;
       }
     });

@@ -61,6 +61,9 @@ struct Span {
   __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : low + (i - sink_tiles); }
 };
 
+// Tiles that hold the tokens below `end`; end + 31 may be past the largest int.
+__device__ __forceinline__ int tiles_up_to(int end) { return end > 0 ? (end - 1) / 32 + 1 : 0; }
+
 __device__ __forceinline__ Span visible_tiles(const AttendArgs &a, int pa, int pb) {
   Span s;
   int end = pb + 1;                                                   // no key from here on
@@ -70,9 +73,9 @@ __device__ __forceinline__ Span visible_tiles(const AttendArgs &a, int pa, int p
   int low = 0;
   if (a.window > 0 && pa >= a.window) low = pa - a.window + 1;
   s.low = low / 32;
-  const int sink_end = (a.sinks + 31) / 32;
+  const int sink_end = tiles_up_to(a.sinks);
   s.sink_tiles = a.window > 0 && sink_end < s.low ? sink_end : s.low;
-  const int last = (end + 31) / 32;
+  const int last = tiles_up_to(end);
   if (end <= 0) {
     s.sink_tiles = 0;
     s.count = 0;

@@ -95,12 +95,15 @@ __global__ __launch_bounds__(256) void owq_cache_append_kernel(AppendArgs a) {
   const CacheView &c = a.c;
   const int b = blockIdx.z, head = blockIdx.y;
   const int row0 = c.starts[b], n_new = c.starts[b + 1] - row0, len = c.lengths[b];
-  const int first = len - n_new, from = first < 0 ? 0 : first;     // position of row 0, first position written
+  const int64_t first = (int64_t)len - n_new;      // position of row 0
+  const int from = first < 0 ? 0 : (int)first;     // first position written
   if (n_new <= 0 || len <= from) return;
   const int tile = from / 32 + (int)blockIdx.x;
-  int t0 = from > tile * 32 ? from - tile * 32 : 0;
-  int t1 = len - tile * 32 < 32 ? len - tile * 32 : 32;             // tokens [t0, t1) of the tile are new
-  const int64_t row_of_tile = (int64_t)row0 + (int64_t)tile * 32 - first;
+  const int64_t token0 = (int64_t)tile * 32;
+  if (token0 >= len) return;
+  int t0 = from > token0 ? (int)(from - token0) : 0;
+  int t1 = len - token0 < 32 ? (int)(len - token0) : 32;            // tokens [t0, t1) of the tile are new
+  const int64_t row_of_tile = row0 + token0 - first;
   if (row_of_tile + t0 < 0) t0 = row_of_tile > -32 ? (int)-row_of_tile : 32;             // rows outside the caller's tensors are not written
   if (row_of_tile + t1 > c.n_rows) t1 = c.n_rows > row_of_tile ? (int)(c.n_rows - row_of_tile) : 0;
   if (t1 <= t0) return;
@@ -223,7 +226,7 @@ int launch_cache_append(const CacheView &c, const void *k, const void *v, int32_
                         int64_t k_head, int64_t v_row, int64_t v_head, void *stream) {
   const AppendArgs a{c, static_cast<const u32 *>(k), static_cast<const u32 *>(v), k_row, k_head, v_row, v_head};
   // max_new tokens touch at most this many tiles, wherever the first of them lies
-  const dim3 grid((unsigned)((max_new + 30) / 32 + 1), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  const dim3 grid((unsigned)(((int64_t)max_new + 30) / 32 + 1), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
   if (type == OWQ_TYPE_F16) owq_cache_append_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   else owq_cache_append_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
@@ -231,7 +234,7 @@ int launch_cache_append(const CacheView &c, const void *k, const void *v, int32_
 
 int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type, int32_t max_len, void *stream) {
   const ReadArgs a{c, static_cast<u32 *>(k_out), static_cast<u32 *>(v_out)};
-  const dim3 grid((unsigned)((max_len + 31) / 32), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  const dim3 grid((unsigned)(((int64_t)max_len + 31) / 32), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
   if (type == OWQ_TYPE_F16) owq_cache_read_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   else owq_cache_read_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();

@@ -531,12 +531,12 @@ def cache_empty(n_pages, page_size, kv_heads, head_dim, device="cuda"):
 
 
 def _cache_args(pages, table, n_seqs, kv_heads, dim):
-    """(description, tokens that a sequence's pages can hold)."""
+    """(description, tokens that a sequence can have on its pages)."""
     n_pages, heads, tiles, size = pages.shape
     rows, stride = table.shape
     assert pages.is_cuda and pages.is_contiguous() and pages.dtype is _TORCH.uint8 and table.is_contiguous() and rows >= n_seqs, (pages.shape, table.shape)
     assert heads == kv_heads and size == 32 * ((dim + 31) // 32 * 32) + 256, (pages.shape, kv_heads, dim)
-    return _CACHE.pack(n_pages, 32 * tiles, heads, dim, n_seqs, stride), 32 * tiles * stride
+    return _CACHE.pack(n_pages, 32 * tiles, heads, dim, n_seqs, stride), min(32 * tiles * stride, 0x7fffffff)
 
 
 def cache_append(pages, page_table, starts, lengths, k, v, max_new=None):

@@ -48,3 +48,19 @@ def test_last_positions(env, new, heads, short_of):      # noqa: F811
     want = step.attention(q.double().cpu().numpy(), np.ascontiguousarray(tiles.transpose(1, 0, 2)[:, :, None]),
                           np.arange(10)[None], [0, new], [cut], dim ** -0.5, window, sinks)
     check(env, *got, want, False)
+
+
+def test_tables_of_more_than_the_largest_length(env):      # noqa: F811
+    # no bound given: the table's capacity, which is more than a length can be
+    torch, B = env
+    rng = np.random.default_rng(43)
+    page, dim = 65536, 16
+    pages = torch.zeros((1, 1, page // 32, step.tile_bytes(dim)), dtype=torch.uint8, device="cuda")
+    table = torch.full((1, 32769), -1, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    args = (table, i32(torch, [0, 40]), i32(torch, [40]))
+    k = torch.from_numpy(rng.normal(size=(40, 1, dim))).half().cuda()
+    B.cache_append(pages, *args, k, k)
+    out, lse = B.cache_attention(k, pages, *args, want_lse=True)
+    want = step.attention(k.double().cpu().numpy(), pages[:, :, :2].cpu().numpy(), np.array([[0]]), [0, 40], [40], dim ** -0.5)
+    check(env, out, lse, want, False)

@@ -9,6 +9,8 @@
 // where a workgroup writes a 32nd of its tile, by latency: 6.5 us and 7.2.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "owq_cache_device.h"
 #include "owq_step.h"
 #include "owq_step_device.h"
@@ -85,6 +87,7 @@ struct AppendArgs {
   CacheView c;
   const u32 *k, *v;
   int64_t k_row, k_head, v_row, v_head;
+  int32_t max_new;
 };
 
 constexpr int kCodePitch = 136;   // bytes of a token's codes in LDS: 128 columns, 8-byte units on other banks
@@ -104,6 +107,7 @@ __global__ __launch_bounds__(256) void owq_cache_append_kernel(AppendArgs a) {
   int t0 = from > token0 ? (int)(from - token0) : 0;
   int t1 = len - token0 < 32 ? (int)(len - token0) : 32;            // tokens [t0, t1) of the tile are new
   const int64_t row_of_tile = row0 + token0 - first;
+  if (first + a.max_new - token0 < t1) t1 = first + a.max_new > token0 ? (int)(first + a.max_new - token0) : 0;   // nor are rows past max_new
   if (row_of_tile + t0 < 0) t0 = row_of_tile > -32 ? (int)-row_of_tile : 32;             // rows outside the caller's tensors are not written
   if (row_of_tile + t1 > c.n_rows) t1 = c.n_rows > row_of_tile ? (int)(c.n_rows - row_of_tile) : 0;
   if (t1 <= t0) return;
@@ -173,6 +177,7 @@ __global__ __launch_bounds__(256) void owq_cache_append_kernel(AppendArgs a) {
 struct ReadArgs {
   CacheView c;
   u32 *k_out, *v_out;
+  int32_t max_len;
 };
 
 template <class E>
@@ -181,7 +186,8 @@ __global__ __launch_bounds__(256) void owq_cache_read_kernel(ReadArgs a) {
   const CacheView &c = a.c;
   const int b = blockIdx.z, head = blockIdx.y, tile = blockIdx.x;
   const int64_t row0 = c.starts[b];
-  const int64_t n = c.starts[b + 1] - row0 - (int64_t)tile * 32;    // tokens wanted from this tile on
+  const int64_t all = c.starts[b + 1] - row0;
+  const int64_t n = (all < a.max_len ? all : a.max_len) - (int64_t)tile * 32;    // tokens wanted from this tile on
   if (n <= 0) return;
   const uint8_t *src = cache_tile(c, b, head, tile);
   const int pad = (c.head_dim + 31) / 32 * 32;
@@ -224,17 +230,18 @@ __global__ __launch_bounds__(256) void owq_cache_read_kernel(ReadArgs a) {
 
 int launch_cache_append(const CacheView &c, const void *k, const void *v, int32_t type, int32_t max_new, int64_t k_row,
                         int64_t k_head, int64_t v_row, int64_t v_head, void *stream) {
-  const AppendArgs a{c, static_cast<const u32 *>(k), static_cast<const u32 *>(v), k_row, k_head, v_row, v_head};
-  // max_new tokens touch at most this many tiles, wherever the first of them lies
-  const dim3 grid((unsigned)(((int64_t)max_new + 30) / 32 + 1), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  const AppendArgs a{c, static_cast<const u32 *>(k), static_cast<const u32 *>(v), k_row, k_head, v_row, v_head, max_new};
+  // so many tokens touch at most this many tiles, wherever the first of them lies
+  const int64_t most = std::min(max_new, c.n_rows);
+  const dim3 grid((unsigned)((most + 30) / 32 + 1), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
   if (type == OWQ_TYPE_F16) owq_cache_append_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   else owq_cache_append_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();
 }
 
 int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type, int32_t max_len, void *stream) {
-  const ReadArgs a{c, static_cast<u32 *>(k_out), static_cast<u32 *>(v_out)};
-  const dim3 grid((unsigned)(((int64_t)max_len + 31) / 32), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
+  const ReadArgs a{c, static_cast<u32 *>(k_out), static_cast<u32 *>(v_out), max_len};
+  const dim3 grid((unsigned)(((int64_t)std::min(max_len, c.n_rows) + 31) / 32), (unsigned)c.kv_heads, (unsigned)c.n_seqs);
   if (type == OWQ_TYPE_F16) owq_cache_read_kernel<F16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   else owq_cache_read_kernel<BF16><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
   return (int)hipGetLastError();

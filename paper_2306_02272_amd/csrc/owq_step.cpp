@@ -111,7 +111,7 @@ owq_status_t owq_cache_append(const owq_cache_desc_t *d, void *pages, const int3
   if (!lengths || !k || !v) return OWQ_ERR_NULL;
   if (!aligned(lengths, 4) || !rows16(k, k_row, k_head) || !rows16(v, v_row, v_head)) return OWQ_ERR_BUFFER;
   const CacheView c = cache_view(*d, pages, page_table, starts, lengths, n_rows);
-  return launch_cache_append(c, k, v, type, std::min(max_new, n_rows), k_row, k_head, v_row, v_head, stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
+  return launch_cache_append(c, k, v, type, max_new, k_row, k_head, v_row, v_head, stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
 }
 
 owq_status_t owq_cache_read(const owq_cache_desc_t *d, const void *pages, const int32_t *page_table, const int32_t *starts,
@@ -126,7 +126,7 @@ owq_status_t owq_cache_read(const owq_cache_desc_t *d, const void *pages, const 
   if (!k_out || !v_out) return OWQ_ERR_NULL;
   if (!aligned(k_out, 16) || !aligned(v_out, 16)) return OWQ_ERR_BUFFER;
   const CacheView c = cache_view(*d, pages, page_table, starts, nullptr, n_rows);
-  return launch_cache_read(c, k_out, v_out, type, std::min(max_len, n_rows), stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
+  return launch_cache_read(c, k_out, v_out, type, max_len, stream) == 0 ? OWQ_OK : OWQ_ERR_HIP;
 }
 
 static owq_status_t check_attention(const owq_cache_desc_t *d, const owq_attention_desc_t *a) {

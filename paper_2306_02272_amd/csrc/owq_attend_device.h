@@ -378,7 +378,8 @@ __device__ __forceinline__ void load_rows(const AttendArgs &a, const Sequence &s
       w.q[n][st] = h;
     }
     w.c1[n] = __builtin_ldexpf(a.scale, 20 - k);
-    w.x1[n] = a.scale * sum;
+    // an infinity makes every score NaN here: by itself it could make them all -infinity, which is a row that sees nothing
+    w.x1[n] = top < __builtin_inff() ? a.scale * sum : __builtin_nanf("");
     w.ref[n] = kNoRef;
     w.l[n] = w.low[n] = 0.f;
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};

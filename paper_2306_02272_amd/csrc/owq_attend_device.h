@@ -37,7 +37,7 @@
 namespace owq {
 
 constexpr int kWaves = 4;
-constexpr float kNoRef = -1e30f;      // finite, so that differences with -infinity stay defined
+constexpr float kNoRef = -3.402823466e38f;   // below every score, finite, so that differences with -infinity stay defined
 constexpr float kRoom = 4.f;          // log2 of the largest p s where the reference has just been raised
 constexpr float kLimit = 2048.f;      // of p s before the reference moves, far inside fp16's range
 

@@ -35,3 +35,28 @@ def test_infinity_against_keys_of_one_sign(env, new, heads, sign, bf16):      # 
     # a row that sees nothing stays 0 and -infinity
     out, lse = B.cache_attention(spoilt, pages, i32(torch, np.full_like(table, -1)), *args[2:], want_lse=True)
     assert (out == 0).all() and torch.isneginf(lse).all()
+
+
+@pytest.mark.parametrize("new,heads", [(1, 1), (3, 2), (90, 1), (80, 128)])
+def test_scores_far_below_zero(env, new, heads):      # noqa: F811
+    # keys that are all alike: every score is the same number near -1e31, and the result the values' mean
+    torch, B = env
+    rng = np.random.default_rng(32)
+    n, dim = 200, 32
+    pages, table = filled(env, rng, [n], heads, dim, 32)
+    k = torch.full((n, heads, dim), 2.0, device="cuda").half()
+    v = torch.from_numpy(rng.normal(size=(n, heads, dim))).half().cuda()
+    args = (pages, i32(torch, table), i32(torch, [0, new]), i32(torch, [n]))
+    B.cache_append(pages, i32(torch, table), i32(torch, [0, n]), i32(torch, [n]), k, v)
+    q = torch.full((new, heads, dim), -2.0 ** 100, device="cuda").to(torch.bfloat16)
+    out, lse = B.cache_attention(q, *args, want_lse=True)
+    score = -2.0 ** 100 * 2 * dim * dim ** -0.5
+    assert ((lse.double() - score).abs() <= 2e-5 * abs(score)).all()
+    _, values = B.cache_read(pages, i32(torch, table), i32(torch, [0, n]), n, dim)
+    sums = values.double().cumsum(0)
+    for i in range(new):
+        seen = n - new + 1 + i
+        mean = sums[seen - 1] / seen
+        # the result's rounding, and fp16 weights on codes 8 from the middle at most
+        tol = 2.0 ** -8 * mean.abs() + 2.0 ** -11 * (values.amax() - values.amin()).double() + 1e-5 * values.abs().max().double()
+        assert ((out[i].double() - mean).abs() <= tol).all()

@@ -327,9 +327,9 @@ static int rope_backward_threads(const owq_rope_desc_t &d, int lanes) {
 // to leave (2048 tokens of 144 heads: 52.5 us with 683 workgroups of three waves, 57.7 with 512, 58.9 with 1024, 86 with 682 of
 // three or four tokens).
 int32_t rope_backward_blocks(const owq_rope_desc_t &d) {
-  const int32_t most = 4096 / (rope_backward_threads(d, rope_lanes(d)) / 64);
-  const int32_t each = (d.n_tokens + most - 1) / most;       // tokens of a workgroup, the same for all but the last
-  return each == 0 ? 0 : (d.n_tokens + each - 1) / each;
+  const int64_t most = 4096 / (rope_backward_threads(d, rope_lanes(d)) / 64);
+  const int64_t each = (d.n_tokens + most - 1) / most;       // tokens of a workgroup, the same for all but the last
+  return each == 0 ? 0 : (int32_t)((d.n_tokens + each - 1) / each);
 }
 
 int launch_rope_backward(const owq_rope_desc_t &d, const RopePtrs &p, void *stream) {

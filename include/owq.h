@@ -489,7 +489,8 @@ owq_status_t owq_cache_read(const owq_cache_desc_t *desc, const void *pages, con
  * or NULL.  A row that sees nothing gets 0 and -infinity.  An infinity or NaN in a query or in
  * a cached head that it sees makes its row NaN; what is masked has no effect, whatever its bits.
  * max_new, max_len: no sequence has more new rows or tokens (rows past max_new are not written,
- * tokens past max_len are not seen); smaller bounds mean fewer empty workgroups.
+ * tokens past max_len are not seen); smaller bounds mean fewer empty workgroups.  Sequences times
+ * key/value heads times blocks of 16 or 32 rows stay below 2^24 (else OWQ_ERR_SHAPE).
  * Scores and sums are fp32; the softmax weights times the values' step sizes are rounded to fp16
  * once (relative 2^-11 per token) for the matrix cores; out is rounded once.
  * workspace: owq_cache_attention_workspace_bytes bytes for the same description and the same

@@ -227,6 +227,7 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   // 32/32 heads, 96 blocks: 72 us, 46 with ranges; 600 of 4000, 152 blocks: 132 us, 122), but for short spans of half a
   // machine's blocks, where a launch to join costs more (3 x 300 of 300, 204 blocks: 18 us, 28 with ranges).
   const int64_t wide = heads * ((rows + 127) / 128);
+  p.fits = true;
   p.many = rows > 64 && (wide >= 256 || (wide >= 128 && tiles <= 16));
   if (p.many) return p;
   p.col_tiles = rows <= 16 ? 1 : 2;
@@ -248,7 +249,9 @@ AttendPlan attend_plan(const owq_cache_desc_t &d, const owq_attention_desc_t &a)
   // ranges of an item cost more to join than they gain (30 000 tokens of 32/8 heads: 21.3 us, 26.1 with 96).
   p.ranges = (int)(2 * items <= resident ? std::min(resident, 32 * items) : 2 * resident);
   // no more workgroups than p.ranges ranges and one more per item; nor than ranges of the least length
-  p.workgroups = (int)(p.whole ? items : std::min(p.ranges + items, items * ((tiles + p.least_tiles - 1) / p.least_tiles)));
+  const int64_t workgroups = p.whole ? items : std::min(p.ranges + items, items * ((tiles + p.least_tiles - 1) / p.least_tiles));
+  p.fits = workgroups * 64 * p.waves < (1ll << 32);      // threads of a launch's axis
+  p.workgroups = p.fits ? (int)workgroups : 0;
   p.slots = p.whole ? 0 : (size_t)p.workgroups * p.slot_rows;
   const int P = (d.head_dim + 31) / 32 * 32;
   p.workspace = p.whole ? 0 : p.slots * (P + 2) * 4 + (size_t)d.n_seqs * 8;

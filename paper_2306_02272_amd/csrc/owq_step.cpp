@@ -152,8 +152,11 @@ owq_status_t owq_cache_attention_workspace_bytes(const owq_cache_desc_t *d, cons
   const owq_status_t st = check_attention(d, a);
   if (st != OWQ_OK) return st;
   if (!bytes) return OWQ_ERR_NULL;
-  *bytes = a->n_rows == 0 || a->max_new == 0 || d->n_seqs == 0 ? 0 : attend_plan(*d, tightened(a)).workspace;
-  return OWQ_OK;
+  *bytes = 0;
+  if (a->n_rows == 0 || a->max_new == 0 || d->n_seqs == 0) return OWQ_OK;
+  const AttendPlan plan = attend_plan(*d, tightened(a));
+  *bytes = plan.workspace;
+  return plan.fits ? OWQ_OK : OWQ_ERR_SHAPE;
 }
 
 owq_status_t owq_cache_attention(const owq_cache_desc_t *d, const owq_attention_desc_t *a, const void *q, const void *pages,
@@ -168,6 +171,7 @@ owq_status_t owq_cache_attention(const owq_cache_desc_t *d, const owq_attention_
   if (!rows16(q, a->q_row, a->q_head) || !aligned(out, 16) || !aligned(lengths, 4) || !aligned(lse, 4)) return OWQ_ERR_BUFFER;
   const owq_attention_desc_t t = tightened(a);
   const AttendPlan plan = attend_plan(*d, t);
+  if (!plan.fits) return OWQ_ERR_SHAPE;
   if (plan.workspace > 0 && !workspace) return OWQ_ERR_NULL;
   if (plan.workspace > 0 && (!aligned(workspace, 256) || workspace_bytes < plan.workspace)) return OWQ_ERR_BUFFER;
   const CacheView c = cache_view(*d, pages, page_table, starts, lengths, a->n_rows);

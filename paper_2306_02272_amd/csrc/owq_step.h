@@ -42,6 +42,7 @@ int launch_cache_read(const CacheView &c, void *k_out, void *v_out, int32_t type
 // The work split of an attention call: everything that follows from the description alone.
 struct AttendPlan {
   int32_t group;        // query heads per key/value head
+  bool fits;            // a launch can hold it
   bool many;            // whole spans of keys for 128 rows; else ranges of them for 16 or 32, and:
   int32_t rows;         // most rows (new tokens x group) of a sequence and key/value head
   int32_t col_tiles;    // 16-row tiles of a wave

@@ -486,13 +486,17 @@ owq_status_t owq_cache_read(const owq_cache_desc_t *desc, const void *pages, con
  * t > p - window or t < sinks:
  *     y_t = scale q . (s_t c_t + lo_t),   out = sum_t softmax(y)_t (s'_t c'_t + lo'_t)
  * out [n_rows][q_heads][head_dim] of `type`, packed; lse fp32 [n_rows][q_heads], ln sum exp y,
- * or NULL.  A row that sees nothing gets 0 and -infinity.  An infinity or NaN in a query or in
- * a cached head that it sees makes its row NaN; what is masked has no effect, whatever its bits.
+ * or NULL.  A row that sees nothing gets 0 and -infinity, any other row with an infinity or NaN
+ * in its query or in a cached head that it sees gets NaN; what is masked has no effect, whatever
+ * its bits.  Rows that belong to no sequence are not written.
  * max_new, max_len: no sequence has more new rows or tokens (rows past max_new are not written,
  * tokens past max_len are not seen); smaller bounds mean fewer empty workgroups.  Sequences times
  * key/value heads times blocks of 16 or 32 rows stay below 2^24 (else OWQ_ERR_SHAPE).
- * Scores and sums are fp32; the softmax weights times the values' step sizes are rounded to fp16
- * once (relative 2^-11 per token) for the matrix cores; out is rounded once.
+ * Sums are held in fp32, scores too, but the matrix cores cut what lies 2^18 below the largest |q|
+ * times a code's step from every product of a score.  The softmax weights times the values' step
+ * sizes are rounded to fp16 (relative 2^-11 per token) for the matrix cores; where the keys are
+ * read for few rows and type is fp16, what that takes away is multiplied too.  out is rounded once.
+ * Scores must be finite in fp32, |q| below 2^118.
  * workspace: owq_cache_attention_workspace_bytes bytes for the same description and the same
  * n_rows, max_new, max_len, q_heads, window and sinks, 256-byte aligned (may be NULL if the
  * answer is 0), contents undefined before and after.
@@ -521,7 +525,7 @@ owq_status_t owq_cache_attention(const owq_cache_desc_t *desc, const owq_attenti
  * token[row] = the one with the largest z - ln e (the lower index of equal ones): each stays
  * with its softmax probability over what is left.  temperature[row] == 0: the largest logit.
  * temperature, top_k, top_p, min_p: [n_rows], or NULL for 1, all, 1, 0; noise may be NULL only
- * if temperature is given, and is read at tokens that stay only.
+ * if temperature is given; only its values at tokens that stay count.
  * logprob[row] (may be NULL) = z[token] - ln sum exp z over the whole vocabulary (with
  * temperature 1 where it is 0).  Logits of -infinity are never chosen.  A row whose largest
  * logit is not finite, or that has a NaN in it, or whose temperature is negative, NaN, infinite or

@@ -2,7 +2,9 @@
 // (sequence, head, block of 16 or 32 rows) has its tiles cut into ranges of equal length, one
 // workgroup each; how long a range is at most goes by the sum of all sequences' tiles, so that the workgroups are as many
 // as the compute units hold at once, whatever the lengths.  A workgroup finds its range by sums over the sequences.  Its
-// waves take tiles in turn and are joined in LDS; ranges are joined by a second launch.
+// waves take tiles in turn and are joined in LDS; ranges are joined by a second launch.  17 to 128 rows leave the most to join:
+// 100 tokens of 3000, 32/8 heads, take 38 us, 30 in 520 workgroups that walk five tiles a wave, 6 to join 10 MB of partial
+// results, where the operations take 4.2 and the bytes 1.0.
 //
 // Bound by memory where there is enough of it: one token each of 64 sequences of 300 to 8192, 32/8 heads of 128, in 76.6 us, 298 MB
 // at 3.9 TB/s.  One token of 40/40 heads behind 4000 takes 17.3 us, 4 of them in the second launch: latency of what a

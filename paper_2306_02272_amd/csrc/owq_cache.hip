@@ -5,8 +5,10 @@
 // rows of the cache's matrix-core words are gathered there (keys: 8 columns of a token, values: 8
 // tokens of a column), so that both sides of the exchange are whole 16- and 8-byte accesses.
 //
-// Bound by memory: four prompts of 7269 tokens together, 40 heads of 128 (148 MB of fp16), in 58 us, back in 34; one token each of 64 sequences,
-// where a workgroup writes a 32nd of its tile, by latency: 6.5 us and 7.2.
+// Four prompts of 7269 tokens together, 40 heads of 128 (148 MB of fp16, 188 with the cache's bytes), in 58 us, 3.2 TB/s: a
+// workgroup asks for its rows only behind lengths and table, and gathers the values' words by single bytes.  Back in 34 us,
+// 5.5 TB/s: bound by memory.  One token each of 64 sequences, where a workgroup writes a 32nd of its tile: 6.7 us, back 7.2, the
+// latency of reads that wait for each other (lengths, table, rows or tile).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -8,8 +8,10 @@
 // (the same for all heads of a token) and walks down the heads.
 //
 // Bound by memory: 4096 tokens of 32 + 8 heads of 128 in 21.1 us, 86 MB at 4.1 TB/s (a copy of 1 GiB runs at 4.77);
-// the gradients of 2048 tokens of 72 + 72 heads in 52.4 us, 4.3 TB/s.  A single token is bound by its call (10.4 us, of
-// them 2.8 in the kernel).
+// the gradients of 2048 tokens of 72 + 72 heads in 52.4 us, 4.3 TB/s, 6 of them for the weights' (sums left by every workgroup
+// and their launch).  1021 tokens of 32 + 32 heads of 80 take 21.1 us, where the bytes take 6.6: 14.8 in the kernel, 9.6 where
+// a workgroup, which has but one token, need not leave sums for the weights, and 3.9 in the second launch.  A single token is
+// bound by its call (10.4 us, of them 2.8 in the kernel).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -323,9 +325,9 @@ static int rope_backward_threads(const owq_rope_desc_t &d, int lanes) {
   return best;
 }
 
-// Four waves per SIMD of 256 compute units at most, and the same number of tokens for each workgroup: every workgroup has sums
-// to leave (2048 tokens of 144 heads: 52.5 us with 683 workgroups of three waves, 57.7 with 512, 58.9 with 1024, 86 with 682 of
-// three or four tokens).
+// 4096 waves at most (156 registers leave room for three per SIMD, 3072), and the same number of tokens for each workgroup, which
+// has sums to leave.  2048 tokens of 144 heads, timed in turn on one set of tensors: 43.8 us with 1024 workgroups of two tokens and
+// three waves, as here; 47.6 with 683 of three tokens, 47.6 with 512 of four, 50.0 with 2048 of one.
 int32_t rope_backward_blocks(const owq_rope_desc_t &d) {
   const int64_t most = 4096 / (rope_backward_threads(d, rope_lanes(d)) / 64);
   const int64_t each = (d.n_tokens + most - 1) / most;       // tokens of a workgroup, the same for all but the last

@@ -537,6 +537,110 @@ owq_status_t owq_sample(const void *logits, int32_t type, int32_t n_rows, int32_
                         const float *noise, int64_t noise_row, const float *temperature, const int32_t *top_k,
                         const float *top_p, const float *min_p, int32_t *token, float *logprob, void *stream);
 
+/*
+ * The ends of a block and of a tuning step: residual sum and norms, dropout, log-probabilities,
+ * with their gradients.  As above no handle is needed, nothing is allocated, copied or waited
+ * for, and results are reproducible bit for bit.  Rows may begin anywhere (pointers on the
+ * boundary of their type); the last axis of every tensor is contiguous, strides count elements.
+ *
+ * Random bits come from Philox 4x32 with ten rounds (Salmon, Moraes, Dror and Shaw, "Parallel
+ * random numbers: as easy as 1, 2, 3", 2011): rng is a pair of 64-bit words in DEVICE memory,
+ * (seed, step); key = (seed's low, high half), counter = (c / 8, row, step's low half, site) for
+ * column c of a row.  Column c has 16 of the four result words' bits: the low half of word
+ * (c % 8) / 2 where c is even, else the high half.  With T = rint(65536 p), an element stays
+ * where its bits are not below T, times 65536 / (65536 - T).  As rng is read when the work runs,
+ * a captured graph drops others on every replay if the step in it is changed in between; site
+ * tells the droppings of one step apart.  p in [0, 65535/65536] (else OWQ_ERR_SHAPE).
+ */
+
+/*
+ * Dropout: out = residual + drop(x) over [n_rows][width], out packed, of `type` (any OWQ_TYPE_*),
+ * in binary32, rounded once; residual may be NULL (0).  Dropped elements are 0 whatever x holds.
+ * The gradient of x is the same call on out's gradient without residual.  out may be x or
+ * residual where that is packed.  With p = 0 rng may be NULL.  No rows or columns: a no-op.
+ */
+owq_status_t owq_dropout(const void *x, const void *residual, int32_t type, int32_t n_rows, int32_t width, int64_t x_row,
+                         int64_t residual_row, const uint64_t *rng, float p, int32_t site, void *out, void *stream);
+
+/*
+ * Residual sum of a block and the norms around it.  With h a row of the residual, o of the
+ * block's output (branch), both of one token:
+ *     u = norm_post(o),  total = h_scale h + branch_scale gate * drop(u),  y = norm(total)
+ *     rms:    n(x) = x / sqrt(mean(x^2) + eps) * weight + bias
+ *     layer:  the same of x - mean(x)
+ * in binary32 throughout, total and y rounded once each (y from the unrounded total).  A norm's
+ * weight and bias may be NULL (1 and 0).  post OWQ_NORM_NONE: u = o.  norm OWQ_NORM_NONE: no y.
+ *   h, total   [n_tokens][width] of h_type: `type`, or OWQ_TYPE_F32; total packed, may be NULL
+ *              (not wanted), may be h where that is packed
+ *   branch, y  [n_tokens][width] of type; branch NULL: total = h_scale h (no gate, post, p then)
+ *   gate       OWQ_GATE_ROW: one row for all tokens; OWQ_GATE_TOKEN: a row per token; of type
+ *   weights, biases [width] of type;  p, site, rng: dropout as above, row = token
+ * type OWQ_TYPE_F16 or OWQ_TYPE_BF16 (else OWQ_ERR_TYPE), width in [1, 16384] (else
+ * OWQ_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op.  A NaN or an infinity stays within its row.
+ *
+ * The backward takes the gradients of y (NULL = none, as without a norm) and of total (NULL =
+ * none), total as the forward left it, and the forward's branch, gate, weights and rng:
+ *     D = dtotal + norm'(dy),  dh = h_scale D,  e = branch_scale D
+ *     dgate = e drop(u),  v = drop(e gate),  dbranch = norm_post'(v)
+ *     norm'(g) = r (q - n mean(q n) - [layer] mean(q)),  q = g weight, n the normalised row, r = 1 / sqrt(..)
+ *     dweight = sum g n,  dbias = sum g over the tokens (of y's and, with v, of the branch's norm)
+ * dh of h_type, dbranch and a token gate's dgate of type, [n_tokens][width] packed; dweight,
+ * dbias, dpost_weight, dpost_bias and a row gate's dgate fp32 [width]; each NULL = not wanted.
+ * branch may be NULL where neither dgate nor a post norm needs it.  dh may be dtotal or total, and
+ * dbranch the branch or dy, where they are packed.  Without tokens the sums are 0.
+ * workspace: owq_residual_norm_backward_workspace_bytes bytes, 16-byte aligned, contents undefined
+ * before and after; it may be NULL if no sum over tokens is wanted.
+ */
+#define OWQ_NORM_NONE 0
+#define OWQ_NORM_RMS 1
+#define OWQ_NORM_LAYER 2
+#define OWQ_GATE_NONE 0
+#define OWQ_GATE_ROW 1
+#define OWQ_GATE_TOKEN 2
+#define OWQ_NORM_MAX_WIDTH 16384
+
+typedef struct {
+  int32_t n_tokens, width, type, h_type;
+  int32_t post, norm, gate, site;
+  float eps, h_scale, branch_scale, p;
+  int64_t h_row, branch_row, gate_row;   /* strides; gate_row counts with OWQ_GATE_TOKEN only */
+  int64_t total_row, dy_row, dtotal_row; /* backward: strides of total and of the incoming gradients */
+} owq_norm_desc_t;
+
+owq_status_t owq_residual_norm(const owq_norm_desc_t *desc, const void *h, const void *branch, const void *gate,
+                               const void *post_weight, const void *post_bias, const void *weight, const void *bias,
+                               const uint64_t *rng, void *total, void *y, void *stream);
+owq_status_t owq_residual_norm_backward_workspace_bytes(const owq_norm_desc_t *desc, size_t *bytes);
+owq_status_t owq_residual_norm_backward(const owq_norm_desc_t *desc, const void *dy, const void *dtotal, const void *total,
+                                        const void *branch, const void *gate, const void *post_weight, const void *post_bias,
+                                        const void *weight, const uint64_t *rng, void *dh, void *dbranch, void *dgate,
+                                        float *dpost_weight, float *dpost_bias, float *dweight, float *dbias, void *workspace,
+                                        size_t workspace_bytes, void *stream);
+
+/*
+ * Log-probabilities of given tokens.  Per row of logits [n_rows][vocab] of `type` (any
+ * OWQ_TYPE_*; row stride logits_row), with z = scale x, m = max x and ln S = ln sum exp(z - scale m):
+ *     logprob = scale (x[target] - m) - ln S          0 where target is outside [0, vocab)
+ *     entropy = ln S - sum p (z - scale m),  p = exp(z - scale m) / S
+ *     top_token, top_logprob [n_rows][top]: the `top` largest logits in descending order, of equal
+ *       ones the lower index first; -1 and -infinity where there are fewer above -infinity
+ * in binary32.  targets int32 [n_rows] or NULL (then logprob is not written and may be NULL);
+ * stats fp32 [3][n_rows] = (m, ln S, entropy), which the backward takes; top in [0, 512].
+ * A row whose largest logit is not finite, or that has a NaN in it, gets NaN (0 for a target
+ * outside), tokens -1.  scale finite and above 0, vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
+ *
+ * The backward: dlogprob, dentropy fp32 [n_rows], either may be NULL (0), alternatives have none,
+ *     dlogits[j] = scale (dlogprob (1[j == target] - p_j) - dentropy p_j (ln p_j + entropy))
+ * of type, packed; dlogits may be logits where that is packed.  A row whose coefficients are
+ * both 0 (dlogprob counts as 0 where the target is outside) gets 0 whatever its logits hold.
+ */
+owq_status_t owq_token_logprobs(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row,
+                                const int32_t *targets, float scale, int32_t top, float *logprob, int32_t *top_token,
+                                float *top_logprob, float *stats, void *stream);
+owq_status_t owq_token_logprobs_backward(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row,
+                                         const int32_t *targets, float scale, const float *stats, const float *dlogprob,
+                                         const float *dentropy, void *dlogits, void *stream);
+
 const char *owq_status_str(owq_status_t s);
 
 #ifdef __cplusplus

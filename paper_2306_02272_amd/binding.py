@@ -26,6 +26,8 @@ STATUS_NAMES = ["OWQ_OK", "OWQ_ERR_NULL", "OWQ_ERR_SHAPE", "OWQ_ERR_BITS", "OWQ_
 OWQ_STATIC_SCRATCH_BYTES = 32 << 20
 OWQ_LAYOUT_GEMV, OWQ_LAYOUT_TILE, OWQ_LAYOUT_COMPACT = 0, 1, 2
 OWQ_TYPE_F16, OWQ_TYPE_BF16, OWQ_TYPE_F32 = 0, 1, 2
+OWQ_NORM_NONE, OWQ_NORM_RMS, OWQ_NORM_LAYER = 0, 1, 2
+OWQ_GATE_NONE, OWQ_GATE_ROW, OWQ_GATE_TOKEN = 0, 1, 2
 
 # every symbol include/owq.h declares
 EXPORTS = ["owq_geometry", "owq_packed_bytes", "owq_pack_host", "owq_unpack_codes", "owq_pack_layer",
@@ -34,7 +36,8 @@ EXPORTS = ["owq_geometry", "owq_packed_bytes", "owq_pack_host", "owq_unpack_code
            "owq_backward_workspace_bytes", "owq_linear_backward", "owq_probe_read", "owq_probe_read_write", "owq_probe_empty", "owq_probe_alu", "owq_probe_mfma", "owq_workspace_bytes", "owq_linear_ws", "owq_linear_static",
            "owq_qk_norm_rope", "owq_qk_norm_rope_backward_workspace_bytes", "owq_qk_norm_rope_backward", "owq_cache_page_bytes",
            "owq_cache_append", "owq_cache_read", "owq_cache_attention_workspace_bytes", "owq_cache_attention",
-           "owq_sample", "owq_status_str"]
+           "owq_sample", "owq_dropout", "owq_residual_norm", "owq_residual_norm_backward_workspace_bytes", "owq_residual_norm_backward",
+           "owq_token_logprobs", "owq_token_logprobs_backward", "owq_status_str"]
 
 
 class OwqError(RuntimeError):
@@ -70,6 +73,12 @@ class CacheDesc(C.Structure):
 class AttentionDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("q_heads", "type", "n_rows", "max_new", "max_len", "window", "sinks")] + \
                [("scale", C.c_float), ("q_row", C.c_int64), ("q_head", C.c_int64)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_tokens", "width", "type", "h_type", "post", "norm", "gate", "site")] + \
+               [(n, C.c_float) for n in ("eps", "h_scale", "branch_scale", "p")] + \
+               [(n, C.c_int64) for n in ("h_row", "branch_row", "gate_row", "total_row", "dy_row", "dtotal_row")]
 
 
 class LayerInfo(C.Structure):
@@ -137,6 +146,13 @@ def lib():
         L.owq_cache_attention_workspace_bytes.argtypes = [P, P, C.POINTER(SZ)]   # takes a c_size_t as it is
         L.owq_cache_attention.argtypes = [P] * 10 + [SZ, P]
         L.owq_sample.argtypes = [P, I32, I32, I32, I64, P, I64] + [P] * 7
+        F32 = C.c_float
+        L.owq_dropout.argtypes = [P, P, I32, I32, I32, I64, I64, P, F32, I32, P, P]
+        L.owq_residual_norm.argtypes = [P] * 12
+        L.owq_residual_norm_backward_workspace_bytes.argtypes = [P, C.POINTER(SZ)]
+        L.owq_residual_norm_backward.argtypes = [P] * 18 + [SZ, P]
+        L.owq_token_logprobs.argtypes = [P, I32, I32, I32, I64, P, F32, I32] + [P] * 5
+        L.owq_token_logprobs_backward.argtypes = [P, I32, I32, I32, I64, P, F32] + [P] * 5
         for n in EXPORTS:
             getattr(L, n).restype = C.c_int
         L.owq_status_str.argtypes = [C.c_int]
@@ -426,12 +442,51 @@ def owq_sample(logits_ptr, type: int, n_rows: int, vocab: int, logits_row: int, 
                             min_p_ptr, token_ptr, logprob_ptr, stream), "owq_sample")
 
 
+def owq_dropout(x_ptr, residual_ptr, type: int, n_rows: int, width: int, x_row: int, residual_row: int, rng_ptr, p: float, site: int, out_ptr,
+                stream: int = 0) -> None:
+    _check(lib().owq_dropout(x_ptr, residual_ptr, type, n_rows, width, x_row, residual_row, rng_ptr, p, site, out_ptr, stream), "owq_dropout")
+
+
+def owq_residual_norm(desc: NormDesc, h_ptr, branch_ptr, gate_ptr, post_weight_ptr, post_bias_ptr, weight_ptr, bias_ptr, rng_ptr, total_ptr,
+                      y_ptr, stream: int = 0) -> None:
+    _check(lib().owq_residual_norm(C.addressof(desc), h_ptr, branch_ptr, gate_ptr, post_weight_ptr, post_bias_ptr, weight_ptr, bias_ptr, rng_ptr,
+                                   total_ptr, y_ptr, stream), "owq_residual_norm")
+
+
+def owq_residual_norm_backward_workspace_bytes(desc: NormDesc) -> int:
+    n = C.c_size_t(0)
+    _check(lib().owq_residual_norm_backward_workspace_bytes(C.addressof(desc), C.byref(n)), "owq_residual_norm_backward_workspace_bytes")
+    return n.value
+
+
+def owq_residual_norm_backward(desc: NormDesc, dy_ptr, dtotal_ptr, total_ptr, branch_ptr, gate_ptr, post_weight_ptr, post_bias_ptr, weight_ptr,
+                               rng_ptr, dh_ptr, dbranch_ptr, dgate_ptr, dpost_weight_ptr, dpost_bias_ptr, dweight_ptr, dbias_ptr,
+                               workspace_ptr, workspace_bytes: int, stream: int = 0) -> None:
+    _check(lib().owq_residual_norm_backward(C.addressof(desc), dy_ptr, dtotal_ptr, total_ptr, branch_ptr, gate_ptr, post_weight_ptr,
+                                            post_bias_ptr, weight_ptr, rng_ptr, dh_ptr, dbranch_ptr, dgate_ptr, dpost_weight_ptr,
+                                            dpost_bias_ptr, dweight_ptr, dbias_ptr, workspace_ptr, workspace_bytes, stream),
+           "owq_residual_norm_backward")
+
+
+def owq_token_logprobs(logits_ptr, type: int, n_rows: int, vocab: int, logits_row: int, targets_ptr, scale: float, top: int, logprob_ptr,
+                       top_token_ptr, top_logprob_ptr, stats_ptr, stream: int = 0) -> None:
+    _check(lib().owq_token_logprobs(logits_ptr, type, n_rows, vocab, logits_row, targets_ptr, scale, top, logprob_ptr, top_token_ptr,
+                                    top_logprob_ptr, stats_ptr, stream), "owq_token_logprobs")
+
+
+def owq_token_logprobs_backward(logits_ptr, type: int, n_rows: int, vocab: int, logits_row: int, targets_ptr, scale: float, stats_ptr,
+                                dlogprob_ptr, dentropy_ptr, dlogits_ptr, stream: int = 0) -> None:
+    _check(lib().owq_token_logprobs_backward(logits_ptr, type, n_rows, vocab, logits_row, targets_ptr, scale, stats_ptr, dlogprob_ptr,
+                                             dentropy_ptr, dlogits_ptr, stream), "owq_token_logprobs_backward")
+
+
 _TORCH = None
 _TYPES = {}
-# the layouts of owq_rope_desc_t, owq_cache_desc_t and owq_attention_desc_t: packed bytes take a fifth of a Structure's time
+# the layouts of owq_rope_desc_t, owq_cache_desc_t, owq_attention_desc_t and owq_norm_desc_t: packed bytes take a fifth of a Structure's time
 _ROPE = struct.Struct("@8ifi8q")
 _CACHE = struct.Struct("@6i")
 _ATTENTION = struct.Struct("@7if2q")
+_NORM = struct.Struct("@8i4f6q")
 
 
 def _torch():
@@ -630,6 +685,187 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
     if status != OWQ_OK:
         raise OwqError(status, "owq_sample")
     return token, logprob
+
+
+def _here(x):
+    """The work goes to the current device's current stream; refuses tensors of another device."""
+    assert x.is_cuda and x.get_device() == _TORCH._C._cuda_getDevice(), x.device
+
+
+def _row_of(x, rows, width, dtype, what):
+    """Address and row stride of a CUDA tensor [rows, width] of `dtype`; (0, 0) for None."""
+    if x is None:
+        return 0, 0
+    row, one = x.stride()
+    assert x.is_cuda and x.dtype is dtype and x.shape == (rows, width) and (one == 1 or width <= 1 or rows == 0), (what, x.dtype, x.shape)
+    return x.data_ptr(), row
+
+
+def _packed(x, rows, width, dtype, what):
+    assert x.is_cuda and x.dtype is dtype and x.shape == (rows, width) and x.is_contiguous(), (what, x.dtype, x.shape)
+    return x
+
+
+def _rng(rng, p):
+    """Address of (seed, step); 0 where nothing is dropped."""
+    if rng is None:
+        assert p == 0.0, "dropout needs a tensor (seed, step)"
+        return 0
+    assert rng.is_cuda and rng.dtype is _TORCH.int64 and rng.is_contiguous() and rng.numel() == 2, (rng.dtype, rng.shape)
+    return rng.data_ptr()
+
+
+def dropout(x, rng, p, site=0, residual=None, out=None):
+    """owq_dropout on CUDA tensors: residual + x with elements dropped with probability p (in 16 bits) and the others divided by the
+    probability to stay, x and residual [rows, width] of one type (fp16, bf16, fp32).  rng: int64 [2], (seed, step), read when the
+    work runs; site: tells the droppings of a step apart.  The gradient of x: the same call on out's gradient, without residual."""
+    torch = _torch()
+    rows, width = x.shape
+    _here(x)
+    x_ptr, x_row = _row_of(x, rows, width, x.dtype, "x")
+    r_ptr, r_row = _row_of(residual, rows, width, x.dtype, "residual")
+    out = x.new_empty((rows, width)) if out is None else _packed(out, rows, width, x.dtype, "out")
+    status = lib().owq_dropout(x_ptr, r_ptr, _type_of(x, OWQ_TYPE_F32), rows, width, x_row, r_row, _rng(rng, p), p, site, out.data_ptr(),
+                               _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_dropout")
+    return out
+
+
+_KINDS = {None: OWQ_NORM_NONE, "rms": OWQ_NORM_RMS, "layer": OWQ_NORM_LAYER}
+
+
+def _vector(x, width, dtype, what):
+    if x is None:
+        return 0
+    assert x.is_cuda and x.dtype is dtype and x.is_contiguous() and x.numel() == width, (what, x.dtype, x.shape)
+    return x.data_ptr()
+
+
+def _gate(gate, tokens, width, dtype):
+    """(kind, address, row stride)"""
+    if gate is None:
+        return OWQ_GATE_NONE, 0, 0
+    if gate.dim() == 1:
+        return OWQ_GATE_ROW, _vector(gate, width, dtype, "gate"), 0
+    return OWQ_GATE_TOKEN, *_row_of(gate, tokens, width, dtype, "gate")
+
+
+def residual_norm(h, branch=None, gate=None, post=None, post_weight=None, post_bias=None, norm="rms", weight=None, bias=None, h_scale=1.0,
+                  branch_scale=1.0, eps=1e-6, rng=None, p=0.0, site=0, want_total=True, out=None):
+    """owq_residual_norm on CUDA tensors: total = h_scale h + branch_scale gate * drop(norm_post(branch)), y = norm(total); returns
+    (total, y), None for what is not wanted (y without a norm).  branch [tokens, width] fp16 or bf16, h the same or fp32, gate [width] or
+    [tokens, width]; post, norm: None, "rms" or "layer", with weights and biases [width] or None; rng, p, site as for dropout.
+    `out`: packed tensors (total, y) to write to, total's may be h."""
+    torch = _torch()
+    tokens, width = h.shape
+    _here(h)
+    dtype = h.dtype if branch is None and weight is None and bias is None else next(t.dtype for t in (branch, weight, bias) if t is not None)
+    if dtype is torch.float32 and out is not None and out[1] is not None:
+        dtype = out[1].dtype
+    h_ptr, h_row = _row_of(h, tokens, width, h.dtype, "h")
+    b_ptr, b_row = _row_of(branch, tokens, width, dtype, "branch")
+    kind, g_ptr, g_row = _gate(gate, tokens, width, dtype)
+    total, y = (None, None) if out is None else out
+    if want_total:
+        total = h.new_empty((tokens, width)) if total is None else _packed(total, tokens, width, h.dtype, "out[0]")
+    else:
+        total = None
+    if norm is None:
+        y = None
+    else:
+        y = h.new_empty((tokens, width), dtype=dtype) if y is None else _packed(y, tokens, width, dtype, "out[1]")
+    desc = _NORM.pack(tokens, width, _TYPES[dtype], _type_of(h, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale, branch_scale, p,
+                      h_row, b_row, g_row, 0, 0, 0)
+    status = lib().owq_residual_norm(desc, h_ptr, b_ptr, g_ptr, _vector(post_weight, width, dtype, "post_weight"),
+                                     _vector(post_bias, width, dtype, "post_bias"), _vector(weight, width, dtype, "weight"),
+                                     _vector(bias, width, dtype, "bias"), _rng(rng, p), _ptr_of(total), _ptr_of(y), _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_residual_norm")
+    return total, y
+
+
+def residual_norm_backward(dy, dtotal, total, branch=None, gate=None, post=None, post_weight=None, post_bias=None, norm="rms", weight=None,
+                           bias=None, h_scale=1.0, branch_scale=1.0, eps=1e-6, rng=None, p=0.0, site=0, workspace=None):
+    """owq_residual_norm_backward: gradients of residual_norm's y and total (either may be None) to its inputs; total as the forward
+    returned it, the others as it took them.  Returns (dh, dbranch, dgate, dpost_weight, dpost_bias, dweight, dbias), None for what is
+    not there; those of weights, biases and a gate [width] are fp32."""
+    torch = _torch()
+    tokens, width = total.shape
+    _here(total)
+    f32 = torch.float32
+    dtype = next((t.dtype for t in (dy, branch, weight) if t is not None), total.dtype)
+    t_ptr, t_row = _row_of(total, tokens, width, total.dtype, "total")
+    dt_ptr, dt_row = _row_of(dtotal, tokens, width, total.dtype, "dtotal")
+    dy_ptr, dy_row = _row_of(dy, tokens, width, dtype, "dy")
+    b_ptr, b_row = _row_of(branch, tokens, width, dtype, "branch")
+    kind, g_ptr, g_row = _gate(gate, tokens, width, dtype)
+    new = total.new_empty
+    shape = (tokens, width)
+    dh = new(shape)
+    dbranch = None if branch is None else new(shape, dtype=dtype)
+    dgate = None if gate is None else new(width, dtype=f32) if kind == OWQ_GATE_ROW else new(shape, dtype=dtype)
+
+    def vector(x, there):
+        return new(width, dtype=f32) if x is not None and there is not None else None
+    dpw, dpb, dw, db = vector(post_weight, post), vector(post_bias, post), vector(weight, norm), vector(bias, norm)
+    _vector(bias, width, dtype, "bias")
+    desc = _NORM.pack(tokens, width, _TYPES[dtype], _type_of(total, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
+                      branch_scale, p, 0, b_row, g_row, t_row, dy_row, dt_row)
+    n = 0
+    if workspace is not None:
+        n = workspace.numel() * workspace.element_size()
+    elif kind == OWQ_GATE_ROW or not (dpw is dpb is dw is db is None):
+        need = C.c_size_t(0)
+        _check(lib().owq_residual_norm_backward_workspace_bytes(desc, C.byref(need)), "owq_residual_norm_backward_workspace_bytes")
+        n = need.value
+        workspace = new(n, dtype=torch.uint8)
+    status = lib().owq_residual_norm_backward(desc, dy_ptr, dt_ptr, t_ptr, b_ptr, g_ptr, _vector(post_weight, width, dtype, "post_weight"),
+                                              _vector(post_bias, width, dtype, "post_bias"), _vector(weight, width, dtype, "weight"),
+                                              _rng(rng, p), dh.data_ptr(), _ptr_of(dbranch), _ptr_of(dgate), _ptr_of(dpw), _ptr_of(dpb),
+                                              _ptr_of(dw), _ptr_of(db), _ptr_of(workspace), n, _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_residual_norm_backward")
+    return dh, dbranch, dgate, dpw, dpb, dw, db
+
+
+def token_logprobs(logits, targets=None, scale=1.0, top=0):
+    """owq_token_logprobs: logits [rows, vocabulary] (fp16, bf16 or fp32), targets int32 [rows] or None, `top` likeliest tokens of
+    every row.  Returns (logprob fp32 [rows] or None, top_token int32 [rows, top] or None, top_logprob fp32 or None, stats fp32
+    [3, rows]): stats are the largest logit, ln sum exp(scale (logit - largest)) and the entropy.  scale = 1 / temperature."""
+    torch = _torch()
+    rows, vocab = logits.shape
+    _here(logits)
+    ptr, row = _row_of(logits, rows, vocab, logits.dtype, "logits")
+    f32 = torch.float32
+    new = logits.new_empty
+    logprob = None if targets is None else new(rows, dtype=f32)
+    top_token, top_logprob = (new((rows, top), dtype=torch.int32), new((rows, top), dtype=f32)) if top else (None, None)
+    stats = new((3, rows), dtype=f32)
+    status = lib().owq_token_logprobs(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, 0 if targets is None else _int32(targets, rows, "targets"),
+                                      scale, top, _ptr_of(logprob), _ptr_of(top_token), _ptr_of(top_logprob), stats.data_ptr(),
+                                      _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_token_logprobs")
+    return logprob, top_token, top_logprob, stats
+
+
+def token_logprobs_backward(dlogprob, dentropy, logits, targets, stats, scale=1.0, out=None):
+    """owq_token_logprobs_backward: gradients fp32 [rows] of the log-probabilities and of the entropies (either may be None) to the
+    logits; targets, stats, scale as in the forward.  Returns dlogits; `out`: where to write them, the logits themselves if packed."""
+    torch = _torch()
+    rows, vocab = logits.shape
+    _here(logits)
+    ptr, row = _row_of(logits, rows, vocab, logits.dtype, "logits")
+    for x, n in ((dlogprob, rows), (dentropy, rows), (stats, 3 * rows)):
+        assert x is None or (x.is_cuda and x.dtype is torch.float32 and x.is_contiguous() and x.numel() == n)
+    out = logits.new_empty((rows, vocab)) if out is None else _packed(out, rows, vocab, logits.dtype, "out")
+    status = lib().owq_token_logprobs_backward(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row,
+                                               0 if targets is None else _int32(targets, rows, "targets"), scale, stats.data_ptr(),
+                                               _ptr_of(dlogprob), _ptr_of(dentropy), out.data_ptr(), _current_stream(torch))
+    if status != OWQ_OK:
+        raise OwqError(status, "owq_token_logprobs_backward")
+    return out
 
 
 class OwqLinear:

@@ -24,9 +24,9 @@ __global__ __launch_bounds__(256) void owq_dropout_kernel(DropoutArgs a, int acr
       float f[8], g[8];
       px.get(f);
       if (a.drop.threshold > 0) {
-        const u32 bits = stays8(a.drop, key, (u32)u, (u32)r);
+        const Stays on(a.drop, key, (u32)u, (u32)r);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = (bits >> j) & 1u ? f[j] * a.drop.scale : 0.f;
+        for (int j = 0; j < 8; ++j) f[j] = on(j) ? f[j] * a.drop.scale : 0.f;
       }
       if (res) {
         pr.get(g);

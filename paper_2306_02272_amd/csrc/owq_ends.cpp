@@ -98,9 +98,9 @@ owq_status_t owq_residual_norm_backward(const owq_norm_desc_t *d, const void *dy
   if (d->gate == OWQ_GATE_NONE) gate = dgate = nullptr;
   NormArgs a = norm_args(d, rng);
   const bool row_gate = d->gate == OWQ_GATE_ROW;
+  const bool branch_side = dbranch || dgate || dpost_weight || dpost_bias;
   if (d->n_tokens > 0) {
     if ((dy && !total) || (d->gate != OWQ_GATE_NONE && !gate) || (a.drop.threshold > 0 && !rng)) return OWQ_ERR_NULL;
-    const bool branch_side = dbranch || dgate || dpost_weight || dpost_bias;
     if (!branch && branch_side && (dgate || d->post != OWQ_NORM_NONE)) return OWQ_ERR_NULL;
   }
   const uintptr_t hs = size_of(d->h_type);
@@ -108,7 +108,9 @@ owq_status_t owq_residual_norm_backward(const owq_norm_desc_t *d, const void *dy
       !aligned(post_weight, 2) || !aligned(post_bias, 2) || !aligned(weight, 2) || !aligned(rng, 8) || !aligned(dbranch, 2) ||
       !aligned(dgate, row_gate ? 4 : 2) || !aligned(dpost_weight, 4) || !aligned(dpost_bias, 4) || !aligned(dweight, 4) || !aligned(dbias, 4))
     return OWQ_ERR_BUFFER;
-  a.dy = dy, a.dtotal = dtotal, a.total = total, a.branch = branch, a.gate = gate;
+  a.dy = dy, a.dtotal = dtotal, a.total = total, a.gate = gate;
+  a.branch = branch_side && (dgate || d->post != OWQ_NORM_NONE) ? branch : nullptr;      // read only where it is needed
+  a.branch_side = branch_side;
   a.post_w = post_weight, a.post_b = post_bias, a.w = weight;
   a.dh = dh, a.dbranch = dbranch, a.dgate = row_gate ? nullptr : dgate;
   float *sums[5] = {};

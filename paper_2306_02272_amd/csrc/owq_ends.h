@@ -34,6 +34,7 @@ struct NormArgs {
   int64_t h_row, branch_row, gate_row, total_row, dy_row, dtotal_row;
   int32_t n_tokens, width, post, norm;
   int32_t n_sums, pitch;
+  int32_t branch_side;                              // backward: something of the branch's is wanted
   int32_t sum_w, sum_b, sum_post_w, sum_post_b, sum_gate;   // which sum is whose, -1 = not wanted
   float eps, h_scale, branch_scale;
   Dropping drop;
@@ -44,6 +45,9 @@ struct NormPlan {
 };
 NormPlan norm_backward_plan(const owq_norm_desc_t &d);
 int launch_norm(const NormArgs &a, int32_t type, int32_t h_type, void *stream);
+// Rows that registers do not hold (owq_norm_wide.hip).
+int launch_norm_wide(const NormArgs &a, int32_t type, int32_t h_type, void *stream);
+void launch_norm_backward_wide(const NormArgs &a, int32_t type, int32_t h_type, int32_t blocks, void *stream);
 // sums: where the sum of each kind goes, in the order of their numbers in a
 int launch_norm_backward(const NormArgs &a, int32_t type, int32_t h_type, const NormPlan &p, float *const *sums, void *stream);
 

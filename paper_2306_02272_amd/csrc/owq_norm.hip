@@ -1,413 +1,463 @@
 // Residual sum of a block with the norms around it, and the gradients.
 //
-// A workgroup takes a row (a token); a thread keeps CH pieces of eight elements of it in registers, so that each input is read
-// once.  A norm needs the row's mean and squares: every wave takes them of its own elements about their own mean (no rounding of
-// a large mean enters), and the waves' are joined as of sets of n_w elements:
+// A team of waves takes a row (a token); a thread keeps CH pieces of eight elements of it in registers, so that each input is
+// read once.  A norm needs the row's mean and squares: every wave takes them of its own elements about their own mean (no
+// rounding of a large mean enters), and the waves' are joined as of sets of n_w elements:
 //     mean = sum n_w mean_w / n,   M = sum M_w + n_w (mean_w - mean)^2
 // which costs one barrier.  Without centring (rms) mean_w = 0 and the same code adds squares.
+//
+// Pieces past the row are 0, and so are weights there, so that products and sums need no further care.
 #include <hip/hip_runtime.h>
 
-#include <mutex>
 #include <type_traits>
 
-#include "owq_random_device.h"
+#include "owq_norm_device.h"
 
 namespace owq {
 
-constexpr int kNormWaves = 16;
+// Most threads of a team, by pieces of a thread: 64 registers for each, or as many as there are.
+constexpr int norm_threads(int ch) { return ch == 1 ? 1024 : ch == 2 ? 640 : 512; }
 
-// Sum over the wave, in every lane.
-__device__ __forceinline__ float wave_sum(float v) {
-  v = wave_scan(v, 0.f, [](float a, float b) { return a + b; });
-  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
-}
-
-template <int CH>
-struct RowPlace {
-  int unit[CH], count[CH];      // pieces of this thread and how many of their elements the row has
-  int wave_count;               // elements of this wave
-  __device__ __forceinline__ RowPlace(int width) {
-    const int first = (threadIdx.x >> 6) * 64;
-    wave_count = 0;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      unit[c] = c * (int)blockDim.x + (int)threadIdx.x;
-      const int n = width - 8 * unit[c], w = width - 8 * (c * (int)blockDim.x + first);
-      count[c] = n < 0 ? 0 : n > 8 ? 8 : n;
-      wave_count += w < 0 ? 0 : w > 512 ? 512 : w;
-    }
-  }
-};
-
-struct RowStat {
-  float mean, size;      // size = 1 / sqrt(mean square + eps)
-};
-
-// What a wave knows of a row: mean and sum of squares about it.
-template <int CH>
-__device__ __forceinline__ void wave_stat(const float (&x)[CH][8], const RowPlace<CH> &at, bool layer, float *mean, float *squares) {
-  float m = 0.f;
-  if (layer) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m += x[c][j];            // 0 past the row
-    m = wave_sum(m) / (float)(at.wave_count > 0 ? at.wave_count : 1);
-  }
-  float s = 0.f;
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float d = j < at.count[c] ? x[c][j] - m : 0.f;
-      s = __builtin_fmaf(d, d, s);
-    }
-  *mean = m;
-  *squares = wave_sum(s);
-}
-
-// Sum over the workgroup's waves of what lane w of every 16 holds for wave w.
-__device__ __forceinline__ float waves_sum(float v) { return lanes_sum<16>(v); }
-
-__device__ __forceinline__ RowStat joined_stat(const float2 *part, int width, int ch, bool layer, float eps) {
-  const int w = threadIdx.x & 15;
-  const bool on = w < (int)(blockDim.x >> 6);
-  const float2 p = on ? part[w] : make_float2(0.f, 0.f);
-  float mean = 0.f, extra = 0.f;
-  if (layer) {
-    int n = 0;
-    for (int c = 0; c < ch; ++c) {
-      const int k = width - 8 * (c * (int)blockDim.x + 64 * w);
-      n += k < 0 ? 0 : k > 512 ? 512 : k;
-    }
-    const float count = on ? (float)n : 0.f;
-    mean = waves_sum(count * p.x) / (float)width;
-    extra = count * (p.x - mean) * (p.x - mean);
-  }
-  const float squares = waves_sum(p.y + extra);
-  return RowStat{mean, 1.f / __builtin_sqrtf(squares / (float)width + eps)};
-}
-
-// Statistics of a row over the whole workgroup.
-template <int CH>
-__device__ __forceinline__ RowStat row_stat(const float (&x)[CH][8], const RowPlace<CH> &at, float2 *part, int width, bool layer, float eps) {
-  float m, s;
-  wave_stat<CH>(x, at, layer, &m, &s);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(m, s);
-  __syncthreads();
-  return joined_stat(part, width, CH, layer, eps);
-}
-
-template <class E, int CH>
-__device__ __forceinline__ void load_row(Piece<E> (&p)[CH], const void *row, const RowPlace<CH> &at, int width) {
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if (row && at.count[c] > 0) p[c].load(row, at.unit[c], width);
-    else p[c].zero();
-  }
-}
-template <class E, int CH>
-__device__ __forceinline__ void store_row(const float (&x)[CH][8], void *row, const RowPlace<CH> &at, int width) {
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    Piece<E> p;
-    p.put(x[c]);
-    if (at.count[c] > 0) p.template store<true>(row, at.unit[c], width);
-  }
-}
-
-// x of a norm's input -> its output; weight and bias as pieces, where there are any
-template <class E, int CH>
-__device__ __forceinline__ void apply_norm(float (&x)[CH][8], const RowStat &s, const Piece<E> (&w)[CH], bool has_w, const Piece<E> (&b)[CH],
-                                           bool has_b) {
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    float g[8];
-    w[c].get(g);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[c][j] = (x[c][j] - s.mean) * s.size;
-      if (has_w) x[c][j] *= g[j];
-    }
-    if (has_b) {
-      b[c].get(g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[c][j] += g[j];
-    }
-  }
-}
-
+// The inputs of a row as they lie in memory.
 template <class E, class H, int CH>
-__global__ __launch_bounds__(1024) void owq_norm_kernel(NormArgs a) {
+struct ForwardRow {
+  Piece<H> h[CH];
+  Piece<E> o[CH], g[CH];
+  __device__ __forceinline__ void load(const NormArgs &a, int64_t t, const RowPlace<CH> &at) {
+    load_row<H, CH>(h, row_at<H>(a.h, t, a.h_row), at, a.width);
+    load_row<E, CH>(o, a.branch ? row_at<E>(a.branch, t, a.branch_row) : nullptr, at, a.width);
+    load_vector<E, CH>(g, a.gate ? row_at<E>(a.gate, t, a.gate_row) : nullptr, 1.f, at, a.width);
+  }
+};
+
+template <class E, class H, int CH, bool POST>
+__global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : POST ? 6 : 8) void owq_norm_kernel(NormArgs a) {
+  constexpr bool AHEAD = CH == 2 && !POST;
   __shared__ float2 part[2][kNormWaves];
-  const RowPlace<CH> at(a.width);
+  const RowPlace<CH> at(a.width, blockDim.x);
+  TeamSum<float2> sums{part[0], 0};
   const DropKey key = drop_key(a.drop);
+  const float inverse_width = 1.f / (float)a.width;
+  const bool layer = a.norm == OWQ_NORM_LAYER, post_layer = a.post == OWQ_NORM_LAYER;
+  ForwardRow<E, H, CH> now, next;
+  if (AHEAD) next.load(a, blockIdx.x, at);
   for (int64_t t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-    Piece<H> ph[CH];
-    Piece<E> po[CH], pg[CH], pw[CH], pb[CH];
-    load_row<H, CH>(ph, row_at<H>(a.h, t, a.h_row), at, a.width);
-    load_row<E, CH>(po, a.branch ? row_at<E>(a.branch, t, a.branch_row) : nullptr, at, a.width);
-    load_row<E, CH>(pg, a.gate ? row_at<E>(a.gate, t, a.gate_row) : nullptr, at, a.width);
+    Piece<E> w[CH], b[CH];
+    if (AHEAD) {
+      now = next;
+      if (t + gridDim.x < a.n_tokens) next.load(a, t + gridDim.x, at);
+    } else {
+      now.load(a, t, at);
+    }
     float x[CH][8];
-    if (a.branch) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) po[c].get(x[c]);
-      if (a.post != OWQ_NORM_NONE) {
-        load_row<E, CH>(pw, a.post_w, at, a.width);
-        load_row<E, CH>(pb, a.post_b, at, a.width);
-        const RowStat s = row_stat<CH>(x, at, part[0], a.width, a.post == OWQ_NORM_LAYER, a.eps);
-        apply_norm<E, CH>(x, s, pw, a.post_w != nullptr, pb, a.post_b != nullptr);
-      }
-      if (a.drop.threshold > 0) {
+    for (int c = 0; c < CH; ++c) now.o[c].get(x[c]);
+    if (POST) {
+      load_vector<E, CH>(w, a.post_w, 1.f, at, a.width);
+      load_vector<E, CH>(b, a.post_b, 0.f, at, a.width);
+      const float2 p = sums.join(at, wave_stat<CH>(x, at, a.width, post_layer), make_float2(0.f, 0.f));
+      apply_norm<E, CH>(x, joined_stat(p, at, inverse_width, post_layer, a.eps), w, b);
+    }
+    if (a.drop.threshold > 0) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const u32 bits = stays8(a.drop, key, (u32)at.unit[c], (u32)t);
+      for (int c = 0; c < CH; ++c) {
+        const Stays on(a.drop, key, (u32)at.unit[c], (u32)t);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[c][j] = (bits >> j) & 1u ? x[c][j] * a.drop.scale : 0.f;
-        }
+        for (int j = 0; j < 8; ++j) x[c][j] = on(j) ? x[c][j] * a.drop.scale : 0.f;
       }
     }
-    load_row<E, CH>(pw, a.w, at, a.width);
-    load_row<E, CH>(pb, a.b, at, a.width);
+    load_vector<E, CH>(w, a.w, 1.f, at, a.width);
+    load_vector<E, CH>(b, a.b, 0.f, at, a.width);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float h[8], g[8];
-      ph[c].get(h);
-      pg[c].get(g);
+      now.h[c].get(h);
+      now.g[c].get(g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float u = a.branch ? a.branch_scale * (a.gate ? x[c][j] * g[j] : x[c][j]) : 0.f;
-        x[c][j] = j < at.count[c] ? __builtin_fmaf(a.h_scale, h[j], u) : 0.f;      // 0 past the row, where a bias may stand
-      }
+      for (int j = 0; j < 8; ++j) x[c][j] = __builtin_fmaf(a.h_scale, h[j], a.branch_scale * (x[c][j] * g[j]));
     }
+    if (AHEAD) loads_done();
     if (a.total_out) store_row<H, CH>(x, row_at<H>(a.total_out, t, a.width), at, a.width);
     if (a.y) {
-      const RowStat s = row_stat<CH>(x, at, part[1], a.width, a.norm == OWQ_NORM_LAYER, a.eps);
-      apply_norm<E, CH>(x, s, pw, a.w != nullptr, pb, a.b != nullptr);
+      const float2 p = sums.join(at, wave_stat<CH>(x, at, a.width, layer), make_float2(0.f, 0.f));
+      apply_norm<E, CH>(x, joined_stat(p, at, inverse_width, layer, a.eps), w, b);
       store_row<E, CH>(x, row_at<E>(a.y, t, a.width), at, a.width);
     }
-    __syncthreads();      // the next row writes `part` again
   }
 }
 
 // ---- gradients ----------------------------------------------------------------------------------------------------------------
-// A workgroup takes rows blockIdx.x, + gridDim.x, ... and adds its part of the sums over tokens to columns that its threads own,
-// in LDS or, where that does not hold them, in its row of the workspace; a second kernel adds the workgroups' in order.
+// With q the gradient of a norm's output times its weight, c the wave's mean and n = (x - mean) size the normalised row, the
+// input's is size (q - n mean(q n) - [layer] mean(q)).  A wave adds q (x - c) and q beside its squares, and the join moves them
+// to the row's mean: sum q (x - mean) = sum_w (Q_w + (c_w - mean) q_w), so that one barrier serves the statistics and both means.
+//
+// A workgroup of at most 1024 threads is as many teams as fit; team i of workgroup k takes rows (k teams + i) + steps of all
+// teams, and asks for its next row before it works on this one (CH = 1).  What it adds up over its rows stays in registers, as a
+// thread owns its columns; at the end the teams' are added through LDS and left as one row of the workspace, which a second
+// kernel adds up in order.  Two pieces a thread leave no registers for that: their sums are kept in LDS, and those that it does
+// not hold in the workspace's row from the start.
 
-// Two sums over the workgroup.
-__device__ __forceinline__ float2 block_sums(float a, float b, float2 *part) {
-  a = wave_sum(a), b = wave_sum(b);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = make_float2(a, b);
-  __syncthreads();
-  const int w = threadIdx.x & 15;
-  const float2 p = w < (int)(blockDim.x >> 6) ? part[w] : make_float2(0.f, 0.f);
-  return make_float2(waves_sum(p.x), waves_sum(p.y));
-}
+// Most threads of a workgroup: 128 registers for a thread, or 168.
+constexpr int norm_backward_threads(int ch, bool branch) { return ch > 1 ? 512 : branch ? 640 : 1024; }
 
-// acc[8 columns] += v
-__device__ __forceinline__ void add_to(float *acc, const float *v) {
-  f32x4 *p = reinterpret_cast<f32x4 *>(acc);
-  const f32x4 a = p[0], b = p[1];
-  p[0] = (f32x4){a[0] + v[0], a[1] + v[1], a[2] + v[2], a[3] + v[3]};
-  p[1] = (f32x4){b[0] + v[4], b[1] + v[5], b[2] + v[6], b[3] + v[7]};
-}
+constexpr int kSumsLds = 38912;      // floats for the sums of two pieces a thread
 
-// Gradient through a norm: q = gradient of its output times the weight (0 past the row), n = normalised row; q becomes the
-// gradient of its input.
+template <int CH, bool REGISTERS>
+struct ColumnSum;
 template <int CH>
-__device__ __forceinline__ void norm_back(float (&q)[CH][8], const float (&n)[CH][8], bool layer, float size, float width, float2 *part) {
-  float qn = 0.f, qs = 0.f;
+struct ColumnSum<CH, true> {
+  float v[CH][8];
+  __device__ __forceinline__ void start(float *, int, int, float *, const RowPlace<CH> &) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      qn = __builtin_fmaf(q[c][j], n[c][j], qn);
-      qs += q[c][j];
+      for (int j = 0; j < 8; ++j) v[c][j] = 0.f;
+  }
+  __device__ __forceinline__ void add(const RowPlace<CH> &, int c, const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[c][j] += x[j];
+  }
+  // store: the workgroup's [teams][columns] in LDS
+  __device__ __forceinline__ void finish(float *mine, int k, int pitch, const RowPlace<CH> &at, int teams, float *store) {
+    if (!mine || k < 0) return;            // the same for the whole workgroup
+    float *to = mine + k * pitch;
+    const int columns = at.threads * 8 * CH;
+    __syncthreads();
+    f32x4 *p = reinterpret_cast<f32x4 *>(store + at.team * columns);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      p[2 * at.unit[c]] = (f32x4){v[c][0], v[c][1], v[c][2], v[c][3]};
+      p[2 * at.unit[c] + 1] = (f32x4){v[c][4], v[c][5], v[c][6], v[c][7]};
     }
-  const float2 s = block_sums(qn, qs, part);
-  const float mn = s.x / width, ms = layer ? s.y / width : 0.f;
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[c][j] = size * (q[c][j] - n[c][j] * mn - ms);
-}
-
-template <class E, class H, int CH, bool LDS>
-__global__ __launch_bounds__(1024) void owq_norm_backward_kernel(NormArgs a) {
-  extern __shared__ __attribute__((aligned(16))) float lds[];
-  __shared__ float2 part[4][kNormWaves];
-  const RowPlace<CH> at(a.width);
-  const DropKey key = drop_key(a.drop);
-  const float width = (float)a.width;
-  float *mine = a.partial ? a.partial + (int64_t)blockIdx.x * a.n_sums * a.pitch : nullptr;
-  float *acc = LDS ? lds : mine;
-  for (int k = 0; k < a.n_sums; ++k)
+    __syncthreads();
+    for (int i = 4 * (int)threadIdx.x; i < pitch; i += 4 * (int)blockDim.x) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < teams; ++j) s += *reinterpret_cast<const f32x4 *>(store + j * columns + i);
+      *reinterpret_cast<f32x4 *>(to + i) = s;
+    }
+  }
+};
+template <int CH>
+struct ColumnSum<CH, false> {
+  float *to;
+  __device__ __forceinline__ void start(float *mine, int k, int pitch, float *store, const RowPlace<CH> &at) {
+    to = !mine || k < 0 ? nullptr : (k + 1) * pitch <= kSumsLds ? store + k * pitch : mine + k * pitch;
+    if (!to) return;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
       if (at.count[c] > 0) {
-        f32x4 *p = reinterpret_cast<f32x4 *>(acc + k * a.pitch + 8 * at.unit[c]);
+        f32x4 *p = reinterpret_cast<f32x4 *>(to) + 2 * at.unit[c];
         p[0] = p[1] = (f32x4){0.f, 0.f, 0.f, 0.f};
       }
-  auto add_row = [&](int k, const float (&v)[CH][8]) {
-    if (k < 0) return;
+  }
+  __device__ __forceinline__ void add(const RowPlace<CH> &at, int c, const float (&x)[8]) {
+    if (!to || at.count[c] == 0) return;
+    f32x4 *p = reinterpret_cast<f32x4 *>(to) + 2 * at.unit[c];
+    const f32x4 a = p[0], b = p[1];
+    p[0] = (f32x4){a[0] + x[0], a[1] + x[1], a[2] + x[2], a[3] + x[3]};
+    p[1] = (f32x4){b[0] + x[4], b[1] + x[5], b[2] + x[6], b[3] + x[7]};
+  }
+  __device__ __forceinline__ void finish(float *mine, int k, int pitch, const RowPlace<CH> &at, int, float *) {
+    if (!mine || k < 0 || (k + 1) * pitch > kSumsLds) return;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
-      if (at.count[c] > 0) add_to(acc + k * a.pitch + 8 * at.unit[c], v[c]);
-  };
-  const bool branch_side = a.dbranch || a.dgate || a.sum_post_w >= 0 || a.sum_post_b >= 0 || a.sum_gate >= 0;
-  const bool need_u = a.dgate || a.sum_gate >= 0, post = a.post != OWQ_NORM_NONE;
-  for (int64_t t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
-    Piece<E> pdy[CH], po[CH], pg[CH], pw[CH];
-    Piece<H> pd[CH], pt[CH];
-    load_row<E, CH>(pdy, a.dy ? row_at<E>(a.dy, t, a.dy_row) : nullptr, at, a.width);
-    load_row<H, CH>(pt, a.dy ? row_at<H>(a.total, t, a.total_row) : nullptr, at, a.width);
-    load_row<H, CH>(pd, a.dtotal ? row_at<H>(a.dtotal, t, a.dtotal_row) : nullptr, at, a.width);
-    load_row<E, CH>(po, branch_side && (post || need_u) ? row_at<E>(a.branch, t, a.branch_row) : nullptr, at, a.width);
-    load_row<E, CH>(pg, a.gate && branch_side ? row_at<E>(a.gate, t, a.gate_row) : nullptr, at, a.width);
-    float d[CH][8], n[CH][8], v[CH][8];
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) d[c][j] = 0.f;
-    if (a.dy) {
-      load_row<E, CH>(pw, a.w, at, a.width);
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        pdy[c].get(d[c]);
-        pt[c].get(n[c]);
+      if (at.count[c] > 0) {
+        const f32x4 *p = reinterpret_cast<const f32x4 *>(to) + 2 * at.unit[c];
+        f32x4 *out = reinterpret_cast<f32x4 *>(mine + k * pitch) + 2 * at.unit[c];
+        out[0] = p[0];
+        out[1] = p[1];
       }
-      const RowStat s = row_stat<CH>(n, at, part[0], a.width, a.norm == OWQ_NORM_LAYER, a.eps);
-      add_row(a.sum_b, d);
+  }
+};
+
+// Sums of a wave: c = its mean (0 without centring), squares of x - c, q (x - c), q.
+template <int CH>
+__device__ __forceinline__ float4 wave_back(const float (&x)[CH][8], const float (&q)[CH][8], const RowPlace<CH> &at, int width, bool layer) {
+  const float2 s = wave_stat<CH>(x, at, width, layer);
+  float qx = 0.f, qs = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) qx = __builtin_fmaf(q[c][j], x[c][j] - s.x, qx);
+  if (layer) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) qs += q[c][j];
+    qs = wave_sum(qs);
+  }
+  return make_float4(s.x, s.y, wave_sum(qx), qs);
+}
+
+template <class E, class H, int CH, bool POST, bool GATED>
+struct BackwardRow {
+  Piece<E> dy[CH], o[CH], g[CH];
+  Piece<H> total[CH], d[CH];
+  // what is not there: 0
+  __device__ __forceinline__ void load(const NormArgs &a, int64_t t, bool on, const RowPlace<CH> &at) {
+    load_row<E, CH>(dy, on && a.dy ? row_at<E>(a.dy, t, a.dy_row) : nullptr, at, a.width);
+    load_row<H, CH>(total, on && a.dy ? row_at<H>(a.total, t, a.total_row) : nullptr, at, a.width);
+    load_row<H, CH>(d, on && a.dtotal ? row_at<H>(a.dtotal, t, a.dtotal_row) : nullptr, at, a.width);
+    if (POST || GATED) load_row<E, CH>(o, on && a.branch ? row_at<E>(a.branch, t, a.branch_row) : nullptr, at, a.width);
+    if (GATED && CH < 3) load_row<E, CH>(g, on ? row_at<E>(a.gate, t, a.gate_row) : nullptr, at, a.width);
+  }
+};
+
+template <class E, class H, int CH, bool POST, bool GATED>
+__global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_norm_backward_kernel(NormArgs a, int team_threads, int teams) {
+  constexpr bool REG = CH == 1, AGAIN = CH > 1;
+  constexpr bool AHEAD = CH < 3 && (!(POST && GATED) || (CH == 1 && Piece<H>::kSize == 2));      // where the registers hold it
+  __shared__ float4 part[2][kNormWaves];
+  __shared__ __attribute__((aligned(16))) float store[REG ? norm_backward_threads(CH, POST || GATED) * 8 : kSumsLds];
+  const RowPlace<CH> at(a.width, team_threads);
+  TeamSum<float4> sums{part[0], 0};
+  const DropKey key = drop_key(a.drop);
+  const float inverse_width = 1.f / (float)a.width;
+  const bool layer = a.norm == OWQ_NORM_LAYER, post_layer = a.post == OWQ_NORM_LAYER;
+  const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+  float *mine = a.partial ? a.partial + (int64_t)blockIdx.x * a.n_sums * a.pitch : nullptr;
+  ColumnSum<CH, REG> sum_w, sum_b, sum_pw, sum_pb, sum_g;
+  sum_w.start(mine, a.sum_w, a.pitch, store, at);
+  sum_b.start(mine, a.sum_b, a.pitch, store, at);
+  if (POST) sum_pw.start(mine, a.sum_post_w, a.pitch, store, at);
+  if (POST) sum_pb.start(mine, a.sum_post_b, a.pitch, store, at);
+  if (GATED) sum_g.start(mine, a.sum_gate, a.pitch, store, at);
+
+  const int64_t stride = (int64_t)gridDim.x * teams;
+  int64_t t = (int64_t)blockIdx.x * teams + at.team;
+  BackwardRow<E, H, CH, POST, GATED> now, next;
+  if (AHEAD) next.load(a, t, t < a.n_tokens, at);
+  // in registers for all rows, or, with three pieces a thread, read again from the caches
+  constexpr bool HELD = CH < 3;
+  Piece<E> w[CH], pw[CH], pb[CH];
+  if (HELD) {
+    load_vector<E, CH>(w, a.w, 1.f, at, a.width);
+    if (POST) load_vector<E, CH>(pw, a.post_w, 1.f, at, a.width);
+    if (POST && GATED) load_vector<E, CH>(pb, a.post_b, 0.f, at, a.width);
+  }
+  auto shared = [&](Piece<E> &p, const void *v, float none, int c, float (&f)[8]) __attribute__((always_inline)) {
+    if (HELD) {
+      again<AGAIN>(p);
+    } else {
+      asm volatile("" : "+s"(v));      // keeps the load in the loop over rows
+      load_shared<E>(p, v, none, at.unit[c], at.count[c], a.width);
+    }
+    p.get(f);
+  };
+  // as long as the workgroup's first team has a row
+  for (int64_t first = (int64_t)blockIdx.x * teams; first < a.n_tokens; first += stride, t += stride) {
+    const bool on_row = t < a.n_tokens;
+    if (AHEAD) {
+      now = next;
+      next.load(a, t + stride, t + stride < a.n_tokens, at);
+    } else {
+      now.load(a, t, on_row, at);
+    }
+    float d[CH][8], n[CH][8], o[CH][8];
+    u32 kept[CH];
+    if (a.dy) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        float w[8];
-        pw[c].get(w);
+        float k[8];
+        now.total[c].get(n[c]);
+        now.dy[c].get(d[c]);
+        sum_b.add(at, c, d[c]);
+        shared(w[c], a.w, 1.f, c, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) d[c][j] *= k[j];
+      }
+      const void *total = row_at<H>(a.total, on_row ? t : 0, a.total_row);
+      if (!HELD) asm volatile("" : "+s"(total));
+      const float4 p = sums.join(at, wave_back<CH>(n, d, at, a.width, layer), none);
+      const BackStat s = joined_back(p, at, inverse_width, layer, a.eps);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        float g[8], y[8], k[8];
+        again<AGAIN>(now.dy[c]);
+        if (!HELD && POST && GATED && Piece<H>::kSize == 4) now.total[c].load(total, at.unit[c], a.width);
+        else again<AGAIN>(now.total[c]);
+        now.dy[c].get(y);
+        now.total[c].get(n[c]);
+        now.d[c].get(g);
+        shared(w[c], a.w, 1.f, c, k);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           n[c][j] = (n[c][j] - s.mean) * s.size;
-          v[c][j] = d[c][j] * n[c][j];
-          if (a.w) d[c][j] *= w[j];
+          d[c][j] = __builtin_fmaf(s.size, y[j] * k[j], g[j]) + __builtin_fmaf(s.along, n[c][j], s.all);
+          y[j] *= n[c][j];
+        }
+        sum_w.add(at, c, y);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) now.d[c].get(d[c]);
+    }
+    if (AHEAD) loads_done();
+    if (a.dh && on_row) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[c][j] = a.h_scale * d[c][j];
+      store_row<H, CH>(n, row_at<H>(a.dh, t, a.width), at, a.width);
+    }
+    if (!a.branch_side) continue;
+    // The branch's side.  n = branch_scale D times what dropping multiplies by, v = the gradient of the norm's output (or of the
+    // branch), which is n gate where it stays.
+    if (POST || GATED) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) now.o[c].get(o[c]);
+    }
+    const float scale = a.branch_scale * a.drop.scale;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      // past the row the norm's means still stand in d
+      if (POST && !GATED && (a.width & 7) != 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[c][j] = j < at.count[c] ? scale * d[c][j] : 0.f;
+      } else {
+        const float f = POST && !GATED && at.count[c] == 0 ? 0.f : scale;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[c][j] = f * d[c][j];
+      }
+      kept[c] = 255u;
+      if (a.drop.threshold > 0) {
+        const Stays on(a.drop, key, (u32)at.unit[c], (u32)t);
+        kept[c] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (GATED) kept[c] |= on(j) ? 1u << j : 0u;
+          else n[c][j] = on(j) ? n[c][j] : 0.f;
         }
       }
-      add_row(a.sum_w, v);
-      norm_back<CH>(d, n, a.norm == OWQ_NORM_LAYER, s.size, width, part[1]);
+    }
+    const void *gate = GATED && !HELD ? row_at<E>(a.gate, t, a.gate_row) : nullptr;      // one team: t is a row
+    const void *branch = POST && GATED && !HELD ? row_at<E>(a.branch, t, a.branch_row) : nullptr;
+    if (!HELD) asm volatile("" : "+s"(branch));
+    auto gradient = [&](int c, float (&v)[8]) __attribute__((always_inline)) {
+      if (GATED) {
+        float g[8];
+        shared(now.g[c], gate, 1.f, c, g);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = n[c][j] * g[j];
+        if (a.drop.threshold > 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = (kept[c] >> j) & 1u ? v[j] : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = n[c][j];
+      }
+    };
+    BackStat s = {0.f, 1.f, 0.f, 0.f};
+    if (POST) {
+      float q[CH][8];
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        float k[8];
+        gradient(c, q[c]);
+        sum_pb.add(at, c, q[c]);
+        shared(pw[c], a.post_w, 1.f, c, k);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[c][j] *= k[j];
+      }
+      const float4 p = sums.join(at, wave_back<CH>(o, q, at, a.width, post_layer), none);
+      s = joined_back(p, at, inverse_width, post_layer, a.eps);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float g[8];
-      pd[c].get(g);
+      float v[8], k[8], f[8];
+      gradient(c, v);
+      if (POST) {
+        if (!HELD && GATED) now.o[c].load(branch, at.unit[c], a.width);
+        else again<AGAIN>(now.o[c]);
+        shared(pw[c], a.post_w, 1.f, c, k);
+        now.o[c].get(o[c]);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        d[c][j] = j < at.count[c] ? d[c][j] + g[j] : 0.f;
-        v[c][j] = a.h_scale * d[c][j];
+        for (int j = 0; j < 8; ++j) o[c][j] = (o[c][j] - s.mean) * s.size;
       }
-    }
-    if (a.dh) store_row<H, CH>(v, row_at<H>(a.dh, t, a.width), at, a.width);
-    if (branch_side) {
-      // d becomes the gradient of u, n the branch normalised
-      RowStat s = {0.f, 1.f};
-      if (post || need_u) {
+      if (GATED) {
+        if (POST) shared(pb[c], a.post_b, 0.f, c, f);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) po[c].get(n[c]);
-        if (post) {
-          s = row_stat<CH>(n, at, part[2], a.width, a.post == OWQ_NORM_LAYER, a.eps);
-          load_row<E, CH>(pw, a.post_w, at, a.width);
+        for (int j = 0; j < 8; ++j) n[c][j] *= POST ? __builtin_fmaf(o[c][j], k[j], f[j]) : o[c][j];
+        if (a.drop.threshold > 0) {      // dropped: 0 whatever the branch holds
+#pragma unroll
+          for (int j = 0; j < 8; ++j) n[c][j] = (kept[c] >> j) & 1u ? n[c][j] : 0.f;
         }
+        sum_g.add(at, c, n[c]);
       }
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const u32 bits = a.drop.threshold > 0 ? stays8(a.drop, key, (u32)at.unit[c], (u32)t) : 255u;
-        float g[8], w[8], b[8];
-        pg[c].get(g);
-        pw[c].get(w);
-        if (need_u && post && a.post_b) {
-          Piece<E> pb;
-          pb.zero();
-          if (at.count[c] > 0) pb.load(a.post_b, at.unit[c], a.width);
-          pb.get(b);
-        }
+      if (POST) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool on = (bits >> j) & 1u;
-          const float e = a.branch_scale * d[c][j];
-          if (post) n[c][j] = (n[c][j] - s.mean) * s.size;
-          if (need_u) {
-            float u = n[c][j];
-            if (post && a.post_w) u *= w[j];
-            if (post && a.post_b) u += b[j];
-            v[c][j] = e * (on ? u * a.drop.scale : 0.f);
-          }
-          const float q = a.gate ? e * g[j] : e;
-          d[c][j] = on ? q * a.drop.scale : 0.f;
+          f[j] = v[j] * o[c][j];
+          v[j] = __builtin_fmaf(s.size, v[j] * k[j], __builtin_fmaf(s.along, o[c][j], s.all));
         }
+        sum_pw.add(at, c, f);
       }
-      if (a.dgate) store_row<E, CH>(v, row_at<E>(a.dgate, t, a.width), at, a.width);
-      add_row(a.sum_gate, v);
-      if (post) {
-        add_row(a.sum_post_b, d);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          float w[8];
-          pw[c].get(w);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            v[c][j] = d[c][j] * n[c][j];
-            if (a.post_w) d[c][j] *= w[j];
-          }
-        }
-        add_row(a.sum_post_w, v);
-        if (a.dbranch) norm_back<CH>(d, n, a.post == OWQ_NORM_LAYER, s.size, width, part[3]);
-      }
-      if (a.dbranch) store_row<E, CH>(d, row_at<E>(a.dbranch, t, a.width), at, a.width);
+      for (int j = 0; j < 8; ++j) d[c][j] = v[j];
     }
-    __syncthreads();      // the next row writes `part` again
+    if (GATED && a.dgate && on_row) store_row<E, CH>(n, row_at<E>(a.dgate, t, a.width), at, a.width);
+    if (a.dbranch && on_row) store_row<E, CH>(d, row_at<E>(a.dbranch, t, a.width), at, a.width);
   }
-  if (LDS && mine)
-    for (int k = 0; k < a.n_sums; ++k)
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (at.count[c] > 0) {
-          const int i = k * a.pitch + 8 * at.unit[c];
-          const f32x4 *from = reinterpret_cast<const f32x4 *>(lds + i);
-          f32x4 *to = reinterpret_cast<f32x4 *>(mine + i);
-          to[0] = from[0];
-          to[1] = from[1];
-        }
+  sum_w.finish(mine, a.sum_w, a.pitch, at, teams, store);
+  sum_b.finish(mine, a.sum_b, a.pitch, at, teams, store);
+  if (POST) sum_pw.finish(mine, a.sum_post_w, a.pitch, at, teams, store);
+  if (POST) sum_pb.finish(mine, a.sum_post_b, a.pitch, at, teams, store);
+  if (GATED) sum_g.finish(mine, a.sum_gate, a.pitch, at, teams, store);
 }
 
 struct NormSums {
   float *out[5];
 };
 
-// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, 16 rows at a time.
+// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, four per thread; 64 rows at a time, four in flight.
 __global__ __launch_bounds__(1024) void owq_norm_sums_kernel(const float *partial, int blocks, int n_sums, int pitch, int width, NormSums sums) {
-  __shared__ float part[16][64];
-  const int lane = threadIdx.x & 63, first = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane, k = blockIdx.y;
-  float v = 0.f;
-  if (col < width)
-    for (int i = first; i < blocks; i += 16) v += partial[((int64_t)i * n_sums + k) * pitch + col];
+  __shared__ f32x4 part[64][16];
+  const int lane = threadIdx.x & 15, first = threadIdx.x >> 4;
+  const int col = blockIdx.x * 64 + 4 * lane, k = blockIdx.y;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (col < pitch) {
+    const float *from = partial + (int64_t)k * pitch + col;
+    const int64_t row = (int64_t)n_sums * pitch;
+    for (int base = 0; base < blocks; base += 256) {
+      f32x4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = base + 64 * j + first;
+        x[j] = *reinterpret_cast<const f32x4 *>(from + (i < blocks ? i : blocks - 1) * row);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (base + 64 * j + first < blocks) v += x[j];
+    }
+  }
   part[first][lane] = v;
   __syncthreads();
-  if (first == 0 && col < width) {
+  if (threadIdx.x < 256) {           // four threads add 16 rows of a column each
+    const int c = threadIdx.x >> 2, q = threadIdx.x & 3;
+    const float *p = reinterpret_cast<const float *>(part);
     float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) total += part[i][lane];
+    for (int i = 0; i < 16; ++i) total += p[(16 * q + i) * 64 + c];
+    total = lanes_sum<4>(total);
     float *out = sums.out[0];
 #pragma unroll
     for (int i = 1; i < 5; ++i) out = k == i ? sums.out[i] : out;
-    out[col] = total;
+    const int at = blockIdx.x * 64 + c;
+    if (q == 0 && at < width) out[at] = total;
   }
 }
 
-// Pieces of a thread and threads of a workgroup.
+// Pieces of a thread and threads of a team.
 struct NormShape {
   int ch, threads;
 };
-static NormShape norm_shape(int width) {
+template <class F>
+static NormShape norm_shape(int width, int pieces, F &&most) {
   const int units = (width + 7) / 8;
-  const int ch = units > 1024 ? 2 : 1;
-  return NormShape{ch, ((units + ch - 1) / ch + 63) / 64 * 64};
+  for (int ch = 1; ch <= pieces; ++ch)
+    if (units <= ch * most(ch)) return NormShape{ch, ((units + ch - 1) / ch + 63) / 64 * 64};
+  return NormShape{0, 0};      // too wide for the registers
 }
 
 template <class F>
@@ -420,41 +470,68 @@ static void for_types(int type, int h_type, F &&f) {
     else f(BF16(), BF16());
   }
 }
+template <class F>
+static void for_bool(bool b, F &&f) {
+  if (b) f(std::true_type());
+  else f(std::false_type());
+}
+template <int MOST, class F>
+static void for_pieces(int ch, F &&f) {
+  if (ch == 1) f(std::integral_constant<int, 1>());
+  else if (ch == 2) f(std::integral_constant<int, 2>());
+  else if constexpr (MOST == 3) f(std::integral_constant<int, 3>());
+}
 
-int launch_norm(const NormArgs &a, int32_t type, int32_t h_type, void *stream) {
-  const NormShape n = norm_shape(a.width);
-  const unsigned grid = (unsigned)(a.n_tokens < (1 << 16) ? a.n_tokens : 1 << 16);
-  const hipStream_t s = static_cast<hipStream_t>(stream);
+int launch_norm(const NormArgs &args, int32_t type, int32_t h_type, void *stream) {
+  NormArgs a = args;
+  if (!a.branch) a.branch_scale = 0.f, a.post = OWQ_NORM_NONE;
+  const NormShape n = norm_shape(a.width, 3, [](int ch) { return norm_threads(ch); });
+  if (n.ch == 0) return launch_norm_wide(a, type, h_type, stream);
+  const int64_t most = n.ch == 1 ? (1 << 20) / n.threads : 256;
+  const unsigned grid = (unsigned)(a.n_tokens < most ? a.n_tokens : most);
   for_types(type, h_type, [&](auto e, auto h) {
-    if (n.ch == 1) owq_norm_kernel<decltype(e), decltype(h), 1><<<grid, n.threads, 0, s>>>(a);
-    else owq_norm_kernel<decltype(e), decltype(h), 2><<<grid, n.threads, 0, s>>>(a);
+    for_pieces<3>(n.ch, [&](auto ch) {
+      for_bool(a.post != OWQ_NORM_NONE, [&](auto post) {
+        owq_norm_kernel<decltype(e), decltype(h), decltype(ch)::value, decltype(post)::value>
+            <<<grid, n.threads, 0, static_cast<hipStream_t>(stream)>>>(a);
+      });
+    });
   });
   return (int)hipGetLastError();
 }
 
+// A workgroup per compute unit; as many teams in it as there are rows for, and the same number of rows for each.
+static NormShape norm_backward_shape(int width, bool branch) {
+  return norm_shape(width, 3, [=](int ch) { return norm_backward_threads(ch, branch); });
+}
+static int norm_teams(const NormShape &n, bool branch, int64_t n_tokens) {
+  const int64_t fit = n.ch != 1 ? 1 : norm_backward_threads(1, branch) / n.threads, rows = (n_tokens + 255) / 256;
+  return (int)(rows < 1 ? 1 : rows < fit ? rows : fit);
+}
+
 NormPlan norm_backward_plan(const owq_norm_desc_t &d) {
-  const int64_t most = 512, each = (d.n_tokens + most - 1) / most;
+  const bool branch = d.post != OWQ_NORM_NONE || d.gate != OWQ_GATE_NONE;
+  const int64_t teams = norm_teams(norm_backward_shape(d.width, branch), branch, d.n_tokens);
+  const int64_t each = (d.n_tokens + 256 * teams - 1) / (256 * teams) * teams;      // rows of a workgroup
   return NormPlan{each == 0 ? 0 : (int32_t)((d.n_tokens + each - 1) / each), (d.width + 7) / 8 * 8};
 }
 
-constexpr int kNormLds = 65536 - 1024;
-
 int launch_norm_backward(const NormArgs &a, int32_t type, int32_t h_type, const NormPlan &p, float *const *sums, void *stream) {
-  const NormShape n = norm_shape(a.width);
+  const bool branch = a.post != OWQ_NORM_NONE || a.gate != nullptr;
+  const NormShape n = norm_backward_shape(a.width, branch);
+  const int teams = norm_teams(n, branch, a.n_tokens);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const int64_t bytes = (int64_t)a.n_sums * p.pitch * 4;
-  const bool lds = bytes <= kNormLds;
-  if (p.blocks > 0) for_types(type, h_type, [&](auto e, auto h) {
-    auto go = [&](auto ch, auto in_lds) {
-      owq_norm_backward_kernel<decltype(e), decltype(h), decltype(ch)::value, decltype(in_lds)::value>
-          <<<p.blocks, n.threads, decltype(in_lds)::value ? (size_t)bytes : 0, s>>>(a);
-    };
-    using One = std::integral_constant<int, 1>;
-    using Two = std::integral_constant<int, 2>;
-    if (n.ch == 1 && lds) go(One(), std::true_type());
-    else if (n.ch == 1) go(One(), std::false_type());
-    else if (lds) go(Two(), std::true_type());
-    else go(Two(), std::false_type());
+  if (p.blocks > 0 && n.ch == 0) {
+    launch_norm_backward_wide(a, type, h_type, p.blocks, stream);
+  } else if (p.blocks > 0) for_types(type, h_type, [&](auto e, auto h) {
+    for_pieces<3>(n.ch, [&](auto ch) {
+      for_bool(a.post != OWQ_NORM_NONE && a.branch_side, [&](auto post) {
+        for_bool(a.gate != nullptr && a.branch_side, [&](auto gated) {
+          owq_norm_backward_kernel<decltype(e), decltype(h), decltype(ch)::value, decltype(post)::value, decltype(gated)::value>
+              <<<p.blocks, n.threads * teams, 0, s>>>(a, n.threads, teams);
+        });
+      });
+    });
   });
   if (a.n_sums > 0) {
     NormSums out{};

@@ -27,22 +27,23 @@ __device__ __forceinline__ u32x4 philox(u32x4 c, u32 k0, u32 k1) {
   return c;
 }
 
-// Which of the elements 8 unit .. 8 unit + 7 of a row stay, one bit each.
-__device__ __forceinline__ u32 stays8(const Dropping &d, const DropKey &k, u32 unit, u32 row) {
-  const u32x4 w = philox((u32x4){unit, row, k.step, (u32)d.site}, k.k0, k.k1);
-  u32 bits = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bits |= (w[i] & 0xffffu) >= d.threshold ? 1u << (2 * i) : 0u;
-    bits |= (w[i] >> 16) >= d.threshold ? 2u << (2 * i) : 0u;
+// Which of the elements 8 unit .. 8 unit + 7 of a row stay.
+struct Stays {
+  u32x4 bits;
+  u32 threshold;
+  __device__ __forceinline__ Stays(const Dropping &d, const DropKey &k, u32 unit, u32 row)
+      : bits(philox((u32x4){unit, row, k.step, (u32)d.site}, k.k0, k.k1)), threshold(d.threshold) {}
+  __device__ __forceinline__ bool operator()(int j) const {
+    const u32 w = bits[j >> 1];
+    return ((j & 1) ? w >> 16 : w & 0xffffu) >= threshold;
   }
-  return bits;
-}
+};
 
 // ---- pieces of eight elements of rows that may begin anywhere -----------------------------------------------------------------
 // The vector loads and stores take addresses on any boundary of the element; the last piece of a row may be cut.
 
 typedef u32x4 u32x4_any2 __attribute__((aligned(2)));
+typedef u32 u32_any2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_any4 __attribute__((aligned(4)));
 
 // The eight elements of a piece as they lie in memory.
@@ -56,11 +57,14 @@ struct Piece {
     const int n = width - 8 * unit;
     if (n >= 8) {
       v = *reinterpret_cast<const u32x4_any2 *>(p);
-    } else {
-      zero();
-#pragma unroll
-      for (int j = 0; j < 7; ++j)
-        if (j < n) v[j >> 1] |= (u32)p[j] << (16 * (j & 1));
+    } else {       // four, two and one
+      const bool four = n > 0 && (n & 4), two = n > 0 && (n & 2), one = n > 0 && (n & 1);
+      u32 a = 0, b = 0, c = 0, d = 0;
+      if (four) a = reinterpret_cast<const u32_any2 *>(p)[0], b = reinterpret_cast<const u32_any2 *>(p)[1];
+      if (two) c = *reinterpret_cast<const u32_any2 *>(p + (four ? 4 : 0));
+      if (one) d = p[(four ? 4 : 0) + (two ? 2 : 0)];
+      const u32 first = two ? c : d, second = two ? d : 0;      // behind the four
+      v = (u32x4){four ? a : first, four ? b : second, four ? first : 0, four ? second : 0};
     }
   }
   __device__ __forceinline__ void get(float *f) const { unpack8<E>(v, f); }
@@ -73,9 +77,11 @@ struct Piece {
       if (KEEP) *reinterpret_cast<u32x4_any2 *>(p) = v;
       else __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any2 *>(p));
     } else {
-#pragma unroll
-      for (int j = 0; j < 7; ++j)
-        if (j < n) p[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+      const bool four = n > 0 && (n & 4), two = n > 0 && (n & 2), one = n > 0 && (n & 1);
+      const u32 first = four ? v[2] : v[0], second = four ? v[3] : v[1];
+      if (four) reinterpret_cast<u32_any2 *>(p)[0] = v[0], reinterpret_cast<u32_any2 *>(p)[1] = v[1];
+      if (two) *reinterpret_cast<u32_any2 *>(p + (four ? 4 : 0)) = first;
+      if (one) p[(four ? 4 : 0) + (two ? 2 : 0)] = (uint16_t)(two ? second : first);
     }
   }
 };
@@ -92,11 +98,17 @@ struct Piece<F32> {
     if (n >= 8) {
       v[0] = reinterpret_cast<const u32x4_any4 *>(p)[0];
       v[1] = reinterpret_cast<const u32x4_any4 *>(p)[1];
-    } else {
-      zero();
-#pragma unroll
-      for (int j = 0; j < 7; ++j)
-        if (j < n) v[j >> 2][j & 3] = p[j];
+    } else {       // four, two and one
+      const bool four = n > 0 && (n & 4), two = n > 0 && (n & 2), one = n > 0 && (n & 1);
+      const u32x4 none = {0, 0, 0, 0};
+      u32x4 a = none;
+      u32 c0 = 0, c1 = 0, d = 0;
+      if (four) a = *reinterpret_cast<const u32x4_any4 *>(p);
+      if (two) c0 = p[four ? 4 : 0], c1 = p[four ? 5 : 1];
+      if (one) d = p[(four ? 4 : 0) + (two ? 2 : 0)];
+      const u32x4 rest = {two ? c0 : d, c1, two ? d : 0, 0};      // behind the four
+      v[0] = four ? a : rest;
+      v[1] = four ? rest : none;
     }
   }
   __device__ __forceinline__ void get(float *f) const {
@@ -121,9 +133,11 @@ struct Piece<F32> {
         else __builtin_nontemporal_store(v[i], reinterpret_cast<u32x4_any4 *>(p) + i);
       }
     } else {
-#pragma unroll
-      for (int j = 0; j < 7; ++j)
-        if (j < n) p[j] = v[j >> 2][j & 3];
+      const bool four = n > 0 && (n & 4), two = n > 0 && (n & 2), one = n > 0 && (n & 1);
+      const u32x4 rest = four ? v[1] : v[0];
+      if (four) *reinterpret_cast<u32x4_any4 *>(p) = v[0];
+      if (two) p[four ? 4 : 0] = rest[0], p[four ? 5 : 1] = rest[1];
+      if (one) p[(four ? 4 : 0) + (two ? 2 : 0)] = two ? rest[2] : rest[0];
     }
   }
 };

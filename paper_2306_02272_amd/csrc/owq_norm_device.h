@@ -6,19 +6,6 @@ namespace owq {
 
 constexpr int kNormWaves = 16;      // of a workgroup
 
-__device__ __forceinline__ float as_float(u32 v) { return __builtin_bit_cast(float, v); }
-
-// Sum over the wave, in every lane, in a fixed order.
-__device__ __forceinline__ float wave_sum(float v) {
-  v = lanes_sum<16>(v);
-  const u32 a = __builtin_bit_cast(u32, v);
-  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
-  v = as_float(r[0]) + as_float(r[1]);
-  const u32 b = __builtin_bit_cast(u32, v);
-  const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
-  return as_float(q[0]) + as_float(q[1]);
-}
-
 // Where a thread's pieces lie: team `team` of the workgroup, `threads` threads and `waves` waves each.
 template <int CH>
 struct RowPlace {
@@ -112,7 +99,7 @@ template <class At>
 __device__ __forceinline__ RowStat joined_stat(float2 p, const At &at, float inverse_width, bool layer, float eps) {
   float mean = 0.f, extra = 0.f;
   if (layer) {
-    mean = lanes_sum<16>(at.join * p.x) * inverse_width;
+    mean = lanes_sum<16>(rounded(at.join * p.x)) * inverse_width;
     extra = at.join * (p.x - mean) * (p.x - mean);
   }
   return RowStat{mean, 1.f / __builtin_sqrtf(lanes_sum<16>(p.y + extra) * inverse_width + eps)};

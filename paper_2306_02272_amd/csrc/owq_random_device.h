@@ -6,6 +6,30 @@
 
 namespace owq {
 
+// A product as it is rounded.  Ahead of a sum over lanes: there the compiler may fuse a lane's own product with the addition,
+// but not its neighbour's, so that lanes would differ in the last bit of a sum that they share.
+__device__ __forceinline__ float rounded(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
+
+// Sum and maximum over the wave, in every lane, in a fixed order.
+template <class F>
+__device__ __forceinline__ float across_rows(float v, F &&f) {
+  const u32 a = __builtin_bit_cast(u32, v);
+  const auto r = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  v = f(__builtin_bit_cast(float, (u32)r[0]), __builtin_bit_cast(float, (u32)r[1]));
+  const u32 b = __builtin_bit_cast(u32, v);
+  const auto q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return f(__builtin_bit_cast(float, (u32)q[0]), __builtin_bit_cast(float, (u32)q[1]));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return across_rows(lanes_sum<16>(v), [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return across_rows(lanes_max<16>(v), [](float a, float b) { return fmaxf(a, b); });
+}
+
 // Halves of the key and the step, read once by a kernel.
 struct DropKey {
   u32 k0, k1, step;

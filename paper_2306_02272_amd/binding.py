@@ -708,9 +708,9 @@ def _packed(x, rows, width, dtype, what):
 
 def _rng(rng, p):
     """Address of (seed, step); 0 where nothing is dropped."""
-    if rng is None:
-        assert p == 0.0, "dropout needs a tensor (seed, step)"
+    if p == 0.0:
         return 0
+    assert rng is not None, "dropout needs a tensor (seed, step)"
     assert rng.is_cuda and rng.dtype is _TORCH.int64 and rng.is_contiguous() and rng.numel() == 2, (rng.dtype, rng.shape)
     return rng.data_ptr()
 
@@ -760,26 +760,34 @@ def residual_norm(h, branch=None, gate=None, post=None, post_weight=None, post_b
     torch = _torch()
     tokens, width = h.shape
     _here(h)
-    dtype = h.dtype if branch is None and weight is None and bias is None else next(t.dtype for t in (branch, weight, bias) if t is not None)
-    if dtype is torch.float32 and out is not None and out[1] is not None:
-        dtype = out[1].dtype
-    h_ptr, h_row = _row_of(h, tokens, width, h.dtype, "h")
-    b_ptr, b_row = _row_of(branch, tokens, width, dtype, "branch")
-    kind, g_ptr, g_row = _gate(gate, tokens, width, dtype)
+    h_dtype = h.dtype
+    dtype = h_dtype
+    if dtype is torch.float32:                     # the type of the rest
+        rest = branch if branch is not None else weight if weight is not None else bias if bias is not None else None if out is None else out[1]
+        dtype = dtype if rest is None else rest.dtype
+    h_ptr, h_row = _row_of(h, tokens, width, h_dtype, "h")
+    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, "branch")
+    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype)
     total, y = (None, None) if out is None else out
-    if want_total:
-        total = h.new_empty((tokens, width)) if total is None else _packed(total, tokens, width, h.dtype, "out[0]")
-    else:
+    if not want_total:
         total = None
+    elif total is None:
+        total = h.new_empty((tokens, width))
+    else:
+        _packed(total, tokens, width, h_dtype, "out[0]")
     if norm is None:
         y = None
+    elif y is None:
+        y = h.new_empty((tokens, width), dtype=dtype)
     else:
-        y = h.new_empty((tokens, width), dtype=dtype) if y is None else _packed(y, tokens, width, dtype, "out[1]")
-    desc = _NORM.pack(tokens, width, _TYPES[dtype], _type_of(h, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale, branch_scale, p,
-                      h_row, b_row, g_row, 0, 0, 0)
-    status = lib().owq_residual_norm(desc, h_ptr, b_ptr, g_ptr, _vector(post_weight, width, dtype, "post_weight"),
-                                     _vector(post_bias, width, dtype, "post_bias"), _vector(weight, width, dtype, "weight"),
-                                     _vector(bias, width, dtype, "bias"), _rng(rng, p), _ptr_of(total), _ptr_of(y), _current_stream(torch))
+        _packed(y, tokens, width, dtype, "out[1]")
+    desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _TYPES.get(h_dtype, 99), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale, branch_scale, p, h_row,
+                      b_row, g_row, 0, 0, 0)
+    status = lib().owq_residual_norm(desc, h_ptr, b_ptr, g_ptr, 0 if post_weight is None else _vector(post_weight, width, dtype, "post_weight"),
+                                     0 if post_bias is None else _vector(post_bias, width, dtype, "post_bias"),
+                                     0 if weight is None else _vector(weight, width, dtype, "weight"),
+                                     0 if bias is None else _vector(bias, width, dtype, "bias"), _rng(rng, p),
+                                     0 if total is None else total.data_ptr(), 0 if y is None else y.data_ptr(), _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_residual_norm")
     return total, y
@@ -810,7 +818,7 @@ def residual_norm_backward(dy, dtotal, total, branch=None, gate=None, post=None,
         return new(width, dtype=f32) if x is not None and there is not None else None
     dpw, dpb, dw, db = vector(post_weight, post), vector(post_bias, post), vector(weight, norm), vector(bias, norm)
     _vector(bias, width, dtype, "bias")
-    desc = _NORM.pack(tokens, width, _TYPES[dtype], _type_of(total, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
+    desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _type_of(total, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
                       branch_scale, p, 0, b_row, g_row, t_row, dy_row, dt_row)
     n = 0
     if workspace is not None:

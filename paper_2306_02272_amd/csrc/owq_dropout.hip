@@ -19,8 +19,10 @@ __global__ __launch_bounds__(256) void owq_dropout_kernel(DropoutArgs a, int acr
     void *out = row_at<E>(a.out, r, a.width);
     for (int u = (int)blockIdx.x * across + (threadIdx.x & (across - 1)); u < units; u += (int)gridDim.x * across) {
       Piece<E> px, pr;
-      px.load(x, u, a.width);
-      if (res) pr.load(res, u, a.width);
+      const int64_t at = (int64_t)u * (8 * Piece<E>::kSize);      // a row may be 2^31 elements long
+      const int left = a.width - 8 * u;
+      px.load(static_cast<const char *>(x) + at, left);
+      if (res) pr.load(static_cast<const char *>(res) + at, left);
       float f[8], g[8];
       px.get(f);
       if (a.drop.threshold > 0) {
@@ -34,7 +36,7 @@ __global__ __launch_bounds__(256) void owq_dropout_kernel(DropoutArgs a, int acr
         for (int j = 0; j < 8; ++j) f[j] += g[j];
       }
       px.put(f);
-      px.template store<false>(out, u, a.width);
+      px.template store<false>(static_cast<char *>(out) + at, left);
     }
   }
 }

@@ -31,10 +31,10 @@ struct ForwardRow {
 };
 
 template <class E, class H, int CH, bool POST>
-__global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : POST ? 6 : 8) void owq_norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : (POST ? 6 : 8) - (Piece<H>::kSize == 4 ? 1 : 0)) void owq_norm_kernel(NormArgs a) {
   constexpr bool AHEAD = CH == 2 && !POST;
   __shared__ float2 part[2][kNormWaves];
-  const RowPlace<CH> at(a.width, blockDim.x);
+  const RowPlace<CH> at(a.width, blockDim.x, true);
   TeamSum<float2> sums{part[0], 0};
   const DropKey key = drop_key(a.drop);
   const float inverse_width = 1.f / (float)a.width;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
   constexpr bool AHEAD = CH < 3 && (!(POST && GATED) || (CH == 1 && Piece<H>::kSize == 2));      // where the registers hold it
   __shared__ float4 part[2][kNormWaves];
   __shared__ __attribute__((aligned(16))) float store[REG ? norm_backward_threads(CH, POST || GATED) * 8 : kSumsLds];
-  const RowPlace<CH> at(a.width, team_threads);
+  const RowPlace<CH> at(a.width, team_threads, false);
   TeamSum<float4> sums{part[0], 0};
   const DropKey key = drop_key(a.drop);
   const float inverse_width = 1.f / (float)a.width;
@@ -410,40 +410,41 @@ struct NormSums {
   float *out[5];
 };
 
-// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, four per thread; 64 rows at a time, four in flight.
+// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, four per thread, four rows of a thread in flight.
 __global__ __launch_bounds__(1024) void owq_norm_sums_kernel(const float *partial, int blocks, int n_sums, int pitch, int width, NormSums sums) {
-  __shared__ f32x4 part[64][16];
-  const int lane = threadIdx.x & 15, first = threadIdx.x >> 4;
-  const int col = blockIdx.x * 64 + 4 * lane, k = blockIdx.y;
+  constexpr int COLS = 64, kLanes = COLS / 4, kRows = 1024 / kLanes;
+  __shared__ f32x4 part[kRows][kLanes];
+  const int lane = threadIdx.x % kLanes, first = threadIdx.x / kLanes;
+  const int col = blockIdx.x * COLS + 4 * lane, k = blockIdx.y;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   if (col < pitch) {
     const float *from = partial + (int64_t)k * pitch + col;
     const int64_t row = (int64_t)n_sums * pitch;
-    for (int base = 0; base < blocks; base += 256) {
+    for (int base = 0; base < blocks; base += 4 * kRows) {
       f32x4 x[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int i = base + 64 * j + first;
+        const int i = base + kRows * j + first;
         x[j] = *reinterpret_cast<const f32x4 *>(from + (i < blocks ? i : blocks - 1) * row);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (base + 64 * j + first < blocks) v += x[j];
+        if (base + kRows * j + first < blocks) v += x[j];
     }
   }
   part[first][lane] = v;
   __syncthreads();
-  if (threadIdx.x < 256) {           // four threads add 16 rows of a column each
+  if (threadIdx.x < 4 * COLS) {           // four threads add a quarter of the rows of a column each
     const int c = threadIdx.x >> 2, q = threadIdx.x & 3;
     const float *p = reinterpret_cast<const float *>(part);
     float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) total += p[(16 * q + i) * 64 + c];
+#pragma unroll 16
+    for (int i = 0; i < kRows / 4; ++i) total += p[(kRows / 4 * q + i) * COLS + c];
     total = lanes_sum<4>(total);
     float *out = sums.out[0];
 #pragma unroll
     for (int i = 1; i < 5; ++i) out = k == i ? sums.out[i] : out;
-    const int at = blockIdx.x * 64 + c;
+    const int at = blockIdx.x * COLS + c;
     if (q == 0 && at < width) out[at] = total;
   }
 }

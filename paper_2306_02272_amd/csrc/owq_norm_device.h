@@ -21,8 +21,8 @@ struct RowPlace {
     }
     return n;
   }
-  __device__ __forceinline__ RowPlace(int width, int team_threads) : threads(team_threads), waves(team_threads >> 6) {
-    team = __builtin_amdgcn_readfirstlane((int)threadIdx.x / threads);      // whole waves
+  __device__ __forceinline__ RowPlace(int width, int team_threads, bool alone) : threads(team_threads), waves(team_threads >> 6) {
+    team = alone ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x / threads);      // whole waves
     const int i = (int)threadIdx.x - team * threads;
     wave = __builtin_amdgcn_readfirstlane(i >> 6);
 #pragma unroll

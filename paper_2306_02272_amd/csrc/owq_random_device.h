@@ -76,9 +76,17 @@ struct Piece {
   static constexpr int kSize = 2;
   u32x4 v;
   __device__ __forceinline__ void zero() { v = (u32x4){0, 0, 0, 0}; }
+  // a row of less than 2^32 bytes: its address and a lane's offset in 32 bits
   __device__ __forceinline__ void load(const void *row, int unit, int width) {
-    const uint16_t *p = static_cast<const uint16_t *>(row) + 8 * unit;
-    const int n = width - 8 * unit;
+    load(static_cast<const char *>(row) + (u32)unit * 16u, width - 8 * unit);
+  }
+  template <bool KEEP>
+  __device__ __forceinline__ void store(void *row, int unit, int width) const {
+    store<KEEP>(static_cast<char *>(row) + (u32)unit * 16u, width - 8 * unit);
+  }
+  // the piece itself, n elements of the row from there on
+  __device__ __forceinline__ void load(const void *piece, int n) {
+    const uint16_t *p = static_cast<const uint16_t *>(piece);
     if (n >= 8) {
       v = *reinterpret_cast<const u32x4_any2 *>(p);
     } else {       // four, two and one
@@ -94,9 +102,8 @@ struct Piece {
   __device__ __forceinline__ void get(float *f) const { unpack8<E>(v, f); }
   __device__ __forceinline__ void put(const float *f) { v = pack8<E>(f); }
   template <bool KEEP>
-  __device__ __forceinline__ void store(void *row, int unit, int width) const {
-    uint16_t *p = static_cast<uint16_t *>(row) + 8 * unit;
-    const int n = width - 8 * unit;
+  __device__ __forceinline__ void store(void *piece, int n) const {
+    uint16_t *p = static_cast<uint16_t *>(piece);
     if (n >= 8) {
       if (KEEP) *reinterpret_cast<u32x4_any2 *>(p) = v;
       else __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any2 *>(p));
@@ -117,8 +124,14 @@ struct Piece<F32> {
   u32x4 v[2];
   __device__ __forceinline__ void zero() { v[0] = v[1] = (u32x4){0, 0, 0, 0}; }
   __device__ __forceinline__ void load(const void *row, int unit, int width) {
-    const u32 *p = static_cast<const u32 *>(row) + 8 * unit;
-    const int n = width - 8 * unit;
+    load(static_cast<const char *>(row) + (u32)unit * 32u, width - 8 * unit);
+  }
+  template <bool KEEP>
+  __device__ __forceinline__ void store(void *row, int unit, int width) const {
+    store<KEEP>(static_cast<char *>(row) + (u32)unit * 32u, width - 8 * unit);
+  }
+  __device__ __forceinline__ void load(const void *piece, int n) {
+    const u32 *p = static_cast<const u32 *>(piece);
     if (n >= 8) {
       v[0] = reinterpret_cast<const u32x4_any4 *>(p)[0];
       v[1] = reinterpret_cast<const u32x4_any4 *>(p)[1];
@@ -147,9 +160,8 @@ struct Piece<F32> {
     for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = __builtin_bit_cast(u32, f[j]);
   }
   template <bool KEEP>
-  __device__ __forceinline__ void store(void *row, int unit, int width) const {
-    u32 *p = static_cast<u32 *>(row) + 8 * unit;
-    const int n = width - 8 * unit;
+  __device__ __forceinline__ void store(void *piece, int n) const {
+    u32 *p = static_cast<u32 *>(piece);
     if (n >= 8) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {

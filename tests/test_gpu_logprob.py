@@ -61,7 +61,7 @@ def check(got, x, targets, scale, top):
         assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
         # d is the log-probability plus ln S
         l = np.broadcast_to((log_s + 2 * U * np.abs(stats[1]))[(...,) + (None,) * (want.ndim - 1)], want.shape)
-        assert (np.abs(got - want)[fine] <= (l + 4 * U * np.abs(want))[fine]).all()
+        assert (np.abs(got[fine] - want[fine]) <= (l + 4 * U * np.abs(want))[fine]).all()
     if targets is None:
         assert lp is None
     else:

@@ -575,8 +575,10 @@ owq_status_t owq_dropout(const void *x, const void *residual, int32_t type, int3
  *   branch, y  [n_tokens][width] of type; branch NULL: total = h_scale h (no gate, post, p then)
  *   gate       OWQ_GATE_ROW: one row for all tokens; OWQ_GATE_TOKEN: a row per token; of type
  *   weights, biases [width] of type;  p, site, rng: dropout as above, row = token
+ *   y may be the branch where that is packed
  * type OWQ_TYPE_F16 or OWQ_TYPE_BF16 (else OWQ_ERR_TYPE), width in [1, 16384] (else
- * OWQ_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op.  A NaN or an infinity stays within its row.
+ * OWQ_ERR_UNSUPPORTED).  n_tokens == 0 is a no-op.  A NaN or an infinity stays within its row (and
+ * reaches the sums over tokens of the backward).
  *
  * The backward takes the gradients of y (NULL = none, as without a norm) and of total (NULL =
  * none), total as the forward left it, and the forward's branch, gate, weights and rng:
@@ -627,7 +629,7 @@ owq_status_t owq_residual_norm_backward(const owq_norm_desc_t *desc, const void 
  * in binary32.  targets int32 [n_rows] or NULL (then logprob is not written and may be NULL);
  * stats fp32 [3][n_rows] = (m, ln S, entropy), which the backward takes; top in [0, 512].
  * A row whose largest logit is not finite, or that has a NaN in it, gets NaN (0 for a target
- * outside), tokens -1.  scale finite and above 0, vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
+ * outside), tokens -1.  scale in [2^-126, 2^126], vocab in [1, 2^24] (else OWQ_ERR_SHAPE).
  *
  * The backward: dlogprob, dentropy fp32 [n_rows], either may be NULL (0), alternatives have none,
  *     dlogits[j] = scale (dlogprob (1[j == target] - p_j) - dentropy p_j (ln p_j + entropy))

@@ -149,7 +149,7 @@ def lib():
         F32 = C.c_float
         L.owq_dropout.argtypes = [P, P, I32, I32, I32, I64, I64, P, F32, I32, P, P]
         L.owq_residual_norm.argtypes = [P] * 12
-        L.owq_residual_norm_backward_workspace_bytes.argtypes = [P, C.POINTER(SZ)]
+        L.owq_residual_norm_backward_workspace_bytes.argtypes = [P, C.POINTER(SZ)]   # takes a c_size_t as it is
         L.owq_residual_norm_backward.argtypes = [P] * 18 + [SZ, P]
         L.owq_token_logprobs.argtypes = [P, I32, I32, I32, I64, P, F32, I32] + [P] * 5
         L.owq_token_logprobs_backward.argtypes = [P, I32, I32, I32, I64, P, F32] + [P] * 5
@@ -801,37 +801,44 @@ def residual_norm_backward(dy, dtotal, total, branch=None, gate=None, post=None,
     torch = _torch()
     tokens, width = total.shape
     _here(total)
-    f32 = torch.float32
-    dtype = next((t.dtype for t in (dy, branch, weight) if t is not None), total.dtype)
-    t_ptr, t_row = _row_of(total, tokens, width, total.dtype, "total")
-    dt_ptr, dt_row = _row_of(dtotal, tokens, width, total.dtype, "dtotal")
-    dy_ptr, dy_row = _row_of(dy, tokens, width, dtype, "dy")
-    b_ptr, b_row = _row_of(branch, tokens, width, dtype, "branch")
-    kind, g_ptr, g_row = _gate(gate, tokens, width, dtype)
-    new = total.new_empty
-    shape = (tokens, width)
+    f32, h_dtype = torch.float32, total.dtype
+    rest = dy if dy is not None else branch if branch is not None else weight
+    dtype = h_dtype if rest is None else rest.dtype
+    t_ptr, t_row = _row_of(total, tokens, width, h_dtype, "total")
+    dt_ptr, dt_row = (0, 0) if dtotal is None else _row_of(dtotal, tokens, width, h_dtype, "dtotal")
+    dy_ptr, dy_row = (0, 0) if dy is None else _row_of(dy, tokens, width, dtype, "dy")
+    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, "branch")
+    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype)
+    new, shape = total.new_empty, (tokens, width)
     dh = new(shape)
     dbranch = None if branch is None else new(shape, dtype=dtype)
-    dgate = None if gate is None else new(width, dtype=f32) if kind == OWQ_GATE_ROW else new(shape, dtype=dtype)
-
-    def vector(x, there):
-        return new(width, dtype=f32) if x is not None and there is not None else None
-    dpw, dpb, dw, db = vector(post_weight, post), vector(post_bias, post), vector(weight, norm), vector(bias, norm)
-    _vector(bias, width, dtype, "bias")
-    desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _type_of(total, OWQ_TYPE_F32), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
+    # the sums over tokens: rows of one tensor, which costs less than one each
+    wanted = (post is not None and post_weight is not None, post is not None and post_bias is not None, norm is not None and weight is not None,
+              norm is not None and bias is not None, kind == OWQ_GATE_ROW)
+    sums = sum(wanted)
+    rows = iter(new((sums, width), dtype=f32).unbind(0) if sums else ())
+    dpw, dpb, dw, db, dgate = [next(rows) if w else None for w in wanted]
+    if kind == OWQ_GATE_TOKEN:
+        dgate = new(shape, dtype=dtype)
+    if bias is not None:
+        _vector(bias, width, dtype, "bias")
+    desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _TYPES.get(h_dtype, 99), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
                       branch_scale, p, 0, b_row, g_row, t_row, dy_row, dt_row)
+    L = lib()
     n = 0
     if workspace is not None:
         n = workspace.numel() * workspace.element_size()
-    elif kind == OWQ_GATE_ROW or not (dpw is dpb is dw is db is None):
+    elif sums:
         need = C.c_size_t(0)
-        _check(lib().owq_residual_norm_backward_workspace_bytes(desc, C.byref(need)), "owq_residual_norm_backward_workspace_bytes")
+        _check(L.owq_residual_norm_backward_workspace_bytes(desc, need), "owq_residual_norm_backward_workspace_bytes")
         n = need.value
         workspace = new(n, dtype=torch.uint8)
-    status = lib().owq_residual_norm_backward(desc, dy_ptr, dt_ptr, t_ptr, b_ptr, g_ptr, _vector(post_weight, width, dtype, "post_weight"),
-                                              _vector(post_bias, width, dtype, "post_bias"), _vector(weight, width, dtype, "weight"),
-                                              _rng(rng, p), dh.data_ptr(), _ptr_of(dbranch), _ptr_of(dgate), _ptr_of(dpw), _ptr_of(dpb),
-                                              _ptr_of(dw), _ptr_of(db), _ptr_of(workspace), n, _current_stream(torch))
+    status = L.owq_residual_norm_backward(desc, dy_ptr, dt_ptr, t_ptr, b_ptr, g_ptr,
+                                          0 if post_weight is None else _vector(post_weight, width, dtype, "post_weight"),
+                                          0 if post_bias is None else _vector(post_bias, width, dtype, "post_bias"),
+                                          0 if weight is None else _vector(weight, width, dtype, "weight"), _rng(rng, p), dh.data_ptr(),
+                                          _ptr_of(dbranch), _ptr_of(dgate), _ptr_of(dpw), _ptr_of(dpb), _ptr_of(dw), _ptr_of(db),
+                                          _ptr_of(workspace), n, _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_residual_norm_backward")
     return dh, dbranch, dgate, dpw, dpb, dw, db
@@ -850,9 +857,10 @@ def token_logprobs(logits, targets=None, scale=1.0, top=0):
     logprob = None if targets is None else new(rows, dtype=f32)
     top_token, top_logprob = (new((rows, top), dtype=torch.int32), new((rows, top), dtype=f32)) if top else (None, None)
     stats = new((3, rows), dtype=f32)
-    status = lib().owq_token_logprobs(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, 0 if targets is None else _int32(targets, rows, "targets"),
-                                      scale, top, _ptr_of(logprob), _ptr_of(top_token), _ptr_of(top_logprob), stats.data_ptr(),
-                                      _current_stream(torch))
+    t_ptr, lp_ptr = (0, 0) if targets is None else (_int32(targets, rows, "targets"), logprob.data_ptr())
+    tt_ptr, tl_ptr = (top_token.data_ptr(), top_logprob.data_ptr()) if top else (0, 0)
+    status = lib().owq_token_logprobs(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, t_ptr, scale, top, lp_ptr, tt_ptr, tl_ptr,
+                                      stats.data_ptr(), _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_token_logprobs")
     return logprob, top_token, top_logprob, stats

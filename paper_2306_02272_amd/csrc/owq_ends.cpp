@@ -139,7 +139,7 @@ owq_status_t owq_residual_norm_backward(const owq_norm_desc_t *d, const void *dy
 static owq_status_t check_logits(int32_t type, int32_t n_rows, int32_t vocab, float scale) {
   if (n_rows < 0 || vocab < 1 || vocab > (1 << 24)) return OWQ_ERR_SHAPE;
   if (type != OWQ_TYPE_F16 && type != OWQ_TYPE_BF16 && type != OWQ_TYPE_F32) return OWQ_ERR_TYPE;
-  return scale > 0.f && std::isfinite(scale) ? OWQ_OK : OWQ_ERR_SHAPE;
+  return scale >= 0x1p-126f && scale <= 0x1p126f ? OWQ_OK : OWQ_ERR_SHAPE;
 }
 
 owq_status_t owq_token_logprobs(const void *logits, int32_t type, int32_t n_rows, int32_t vocab, int64_t logits_row,

@@ -246,7 +246,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
   };
   // as long as the workgroup's first team has a row
   for (int64_t first = (int64_t)blockIdx.x * teams; first < a.n_tokens; first += stride, t += stride) {
-    const bool on_row = t < a.n_tokens;
+    const bool on_row = t < a.n_tokens;      // else a team without one: zeros, which without eps are no numbers once normalised
     if (AHEAD) {
       now = next;
       next.load(a, t + stride, t + stride < a.n_tokens, at);
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
         float k[8];
         now.total[c].get(n[c]);
         now.dy[c].get(d[c]);
-        sum_b.add(at, c, d[c]);
+        if (on_row) sum_b.add(at, c, d[c]);
         shared(w[c], a.w, 1.f, c, k);
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[c][j] *= k[j];
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
           d[c][j] = __builtin_fmaf(s.size, y[j] * k[j], g[j]) + __builtin_fmaf(s.along, n[c][j], s.all);
           y[j] *= n[c][j];
         }
-        sum_w.add(at, c, y);
+        if (on_row) sum_w.add(at, c, y);
       }
     } else {
 #pragma unroll
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
       for (int c = 0; c < CH; ++c) {
         float k[8];
         gradient(c, q[c]);
-        sum_pb.add(at, c, q[c]);
+        if (on_row) sum_pb.add(at, c, q[c]);
         shared(pw[c], a.post_w, 1.f, c, k);
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[c][j] *= k[j];
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
 #pragma unroll
           for (int j = 0; j < 8; ++j) n[c][j] = (kept[c] >> j) & 1u ? n[c][j] : 0.f;
         }
-        sum_g.add(at, c, n[c]);
+        if (on_row) sum_g.add(at, c, n[c]);
       }
       if (POST) {
 #pragma unroll
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(norm_backward_threads(CH, POST || GATED)) void owq_
           f[j] = v[j] * o[c][j];
           v[j] = __builtin_fmaf(s.size, v[j] * k[j], __builtin_fmaf(s.along, o[c][j], s.all));
         }
-        sum_pw.add(at, c, f);
+        if (on_row) sum_pw.add(at, c, f);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[c][j] = v[j];

@@ -94,7 +94,7 @@ def test_norm_backward_pointers(lib):
 
 @pytest.mark.parametrize("kw,want", [
     (dict(n_rows=-1), B.OWQ_ERR_SHAPE), (dict(vocab=0), B.OWQ_ERR_SHAPE), (dict(vocab=(1 << 24) + 1), B.OWQ_ERR_SHAPE), (dict(type=3), B.OWQ_ERR_TYPE),
-    (dict(scale=0.0), B.OWQ_ERR_SHAPE), (dict(scale=-1.0), B.OWQ_ERR_SHAPE), (dict(scale=INF), B.OWQ_ERR_SHAPE), (dict(scale=NAN), B.OWQ_ERR_SHAPE),
+    (dict(scale=0.0), B.OWQ_ERR_SHAPE), (dict(scale=-1.0), B.OWQ_ERR_SHAPE), (dict(scale=3e38), B.OWQ_ERR_SHAPE), (dict(scale=1e-39), B.OWQ_ERR_SHAPE), (dict(scale=INF), B.OWQ_ERR_SHAPE), (dict(scale=NAN), B.OWQ_ERR_SHAPE),
     (dict(logits=0), B.OWQ_ERR_NULL), (dict(stats=0), B.OWQ_ERR_NULL), (dict(logits=P + 1), B.OWQ_ERR_BUFFER), (dict(logits=P + 2, type=2), B.OWQ_ERR_BUFFER),
     (dict(targets=P + 2), B.OWQ_ERR_BUFFER), (dict(stats=P + 2), B.OWQ_ERR_BUFFER), (dict(n_rows=0, logits=0), B.OWQ_OK)])
 def test_logprobs(lib, kw, want):

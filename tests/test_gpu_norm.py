@@ -314,3 +314,45 @@ def test_more_tokens_than_workgroups_in_turn(env):
     h = torch.randn(70001, 16, device="cuda").half()
     y = host(B.residual_norm(h, eps=EPS)[1])
     close(y, ends.norm(host(h), "rms", None, None, EPS), "float16", 4e-6)
+
+
+@pytest.mark.parametrize("post,gate", [(None, None), ("layer", None), ("rms", "row"), (None, "token")])
+def test_teams_without_a_row_add_nothing(env, post, gate):
+    # two teams a workgroup and an odd number of rows: the last team has none, and without eps a row of zeros is no number
+    torch, B = env
+    g = torch.Generator("cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").half()  # noqa: E731
+    rows, width = 301, 72
+    total, branch, dy, dt = (rand(rows, width) for _ in range(4))
+    options = dict(gate=None if gate is None else rand(width) if gate == "row" else rand(rows, width), post=post, post_weight=rand(width) if post else None,
+                   norm="layer", weight=rand(width), bias=rand(width), eps=0.0)
+    _, dbranch, dgate, dpw, _, dw, db = B.residual_norm_backward(dy, dt, total, branch, **options)
+    want = ends.residual_norm_backward(host(dy), host(dt), host(total), host(branch), host(options["gate"]), post, host(options["post_weight"]), None,
+                                       "layer", host(options["weight"]), 1.0, 1.0, 0.0)
+    for got, terms in ((dw, want["w"]), (db, want["b"]), (dpw, want.get("post_w")), (dgate if gate == "row" else None, want.get("gate"))):
+        if got is not None:
+            # against the terms' sizes: twelve roundings of a row's statistics and sums (2^-24 each) and 64 additions
+            assert (np.abs(host(got) - terms.sum(0)) <= 1.2e-5 * np.abs(terms).max(1, keepdims=True).sum(0) * np.ones(width) + 1e-5 * np.abs(terms).sum(0)).all()
+    assert torch.isfinite(dbranch).all()
+
+
+def test_offsets_past_32_bits(env):
+    # rows that lie further apart than 2^31 bytes: bit for bit what packed rows give
+    torch, B = env
+    rows, width, stride = 4, 200, 2 ** 30 + 3
+
+    def far():
+        return torch.zeros((rows - 1) * stride + width, dtype=torch.float16, device="cuda").as_strided((rows, width), (stride, 1)).normal_()
+    h, branch = far(), far()
+    w = (1 + 0.1 * torch.randn(width, device="cuda")).half()
+    key = torch.tensor([1, 2], dtype=torch.int64, device="cuda")
+    options = dict(norm="layer", weight=w, post="rms", rng=key, p=0.2)
+    got = B.residual_norm(h, branch, **options)
+    want = B.residual_norm(h.contiguous(), branch.contiguous(), **options)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    got = B.residual_norm_backward(branch, h, h, branch, **options)
+    packed = h.contiguous(), branch.contiguous()
+    want = B.residual_norm_backward(packed[1], packed[0], packed[0], packed[1], **options)
+    for a, b in zip(got, want):
+        assert (a is None) == (b is None) and (a is None or torch.equal(a, b))
+    assert torch.equal(B.dropout(h, key, 0.3, residual=branch), B.dropout(packed[0], key, 0.3, residual=packed[1]))

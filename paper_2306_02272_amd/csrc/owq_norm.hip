@@ -7,6 +7,13 @@
 // which costs one barrier.  Without centring (rms) mean_w = 0 and the same code adds squares.
 //
 // Pieces past the row are 0, and so are weights there, so that products and sums need no further care.
+//
+// What bounds it, with the rows' bytes at the rate of a large copy (5.1 TB/s) in brackets: one row of 4096 3.3 us (a load, a
+// reduction, a store behind each other); 4096 rows of 4096 fp16, layer norm, 24 to 28 us (26.3; reads and writes of memory); 1021
+// rows of 9216 with both norms and the gate, fp32 residual, 26 to 32 (22.2; 84 registers, nine waves per compute unit's
+// workgroup).  Gradients: 4096 rows of 4096 with dropout 34 + 4 us (32.9: memory, and 8 MB of partial sums written and read);
+// 777 rows of 5003 with both norms and the gate 30 + 4 (9.2: ten waves per compute unit, one row behind the other in each;
+// vector instructions take a quarter of the cycles).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -15,7 +22,10 @@
 
 namespace owq {
 
-// Most threads of a team, by pieces of a thread: 64 registers for each, or as many as there are.
+// Most threads of a team, by pieces of a thread: 64 registers for each, or as many as there are.  Fewest pieces first: 3640 rows of
+// 4608 take 29 us with one piece and 45 with two (both norms 45 and 60), rows of 8192 29.4 and 30.5.  Past three pieces the rolled
+// kernels: 1021 rows of 9216 19.4 us with two pieces and 19.7 in a rolled one (both norms 32.4 and 42.9),
+// 1021 of 11 008 with two norms 32.7 with three and 43.0.
 constexpr int norm_threads(int ch) { return ch == 1 ? 1024 : ch == 2 ? 640 : 512; }
 
 // The inputs of a row as they lie in memory.
@@ -32,7 +42,7 @@ struct ForwardRow {
 
 template <class E, class H, int CH, bool POST>
 __global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : (POST ? 6 : 8) - (Piece<H>::kSize == 4 ? 1 : 0)) void owq_norm_kernel(NormArgs a) {
-  constexpr bool AHEAD = CH == 2 && !POST;
+  constexpr bool AHEAD = CH == 2 && !POST;      // where the registers hold the next row: 1021 rows of 9216 19.4 us, 25.4 by workgroups of a row
   __shared__ float2 part[2][kNormWaves];
   const RowPlace<CH> at(a.width, blockDim.x, true);
   TeamSum<float2> sums{part[0], 0};
@@ -97,7 +107,9 @@ __global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : (POST ? 6 : 8) - (Pi
 // kernel adds up in order.  Two pieces a thread leave no registers for that: their sums are kept in LDS, and those that it does
 // not hold in the workspace's row from the start.
 
-// Most threads of a workgroup: 128 registers for a thread, or 168.
+// Most threads of a workgroup: 128 registers for a thread, or 168 with the branch's side.  1021 rows of 8192 with both norms and the
+// gate take 48.8 us with two pieces a thread, 76 in the rolled kernel; 1021 of 11 008 45 with three (rms before, no gate) and 58; 2048 of
+// 8192 without the branch's side 38.0 with one piece and 1024 threads, 43.1 with two and 512.
 constexpr int norm_backward_threads(int ch, bool branch) { return ch > 1 ? 512 : branch ? 640 : 1024; }
 
 constexpr int kSumsLds = 38912;      // floats for the sums of two pieces a thread
@@ -410,7 +422,9 @@ struct NormSums {
   float *out[5];
 };
 
-// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, four per thread, four rows of a thread in flight.
+// Column sums of partial [blocks][n_sums][pitch]: 64 columns per workgroup, four per thread, four rows of a thread in flight.  4.0 us for
+// 8 MB of 256 workgroups' two sums of 4096, which lie in the last-level cache: the launch, two loads behind each other, a barrier.
+// 32 columns or 16 per workgroup were no faster.
 __global__ __launch_bounds__(1024) void owq_norm_sums_kernel(const float *partial, int blocks, int n_sums, int pitch, int width, NormSums sums) {
   constexpr int COLS = 64, kLanes = COLS / 4, kRows = 1024 / kLanes;
   __shared__ f32x4 part[kRows][kLanes];
@@ -488,7 +502,13 @@ int launch_norm(const NormArgs &args, int32_t type, int32_t h_type, void *stream
   if (!a.branch) a.branch_scale = 0.f, a.post = OWQ_NORM_NONE;
   const NormShape n = norm_shape(a.width, 3, [](int ch) { return norm_threads(ch); });
   if (n.ch == 0) return launch_norm_wide(a, type, h_type, stream);
-  const int64_t most = n.ch == 1 ? (1 << 20) / n.threads : 256;
+  // As many workgroups as the registers let be at work together, each of which takes several rows, where rows wait for a norm of the
+  // branch or fill most of a compute unit: 3640 rows of 4608 with both norms 38.6 us, 45.2 with more workgroups than that; 2340 of
+  // 7168 29.2 and 33.4.  Otherwise new workgroups as others end, whose loads run beside those: 5000 rows of 2560 24.3, 27.9 so.
+  // With two or three pieces one workgroup per compute unit: 1021 rows of 9216 19.4 us, 21.0 with two.
+  const int waves = 4 * ((a.post != OWQ_NORM_NONE ? 6 : 8) - (h_type == OWQ_TYPE_F32 ? 1 : 0)), per_row = n.threads / 64;
+  const bool resident = a.post != OWQ_NORM_NONE || per_row >= 12;
+  const int64_t most = n.ch > 1 ? 256 : resident ? 256 * (waves / per_row) : (1 << 20) / n.threads;
   const unsigned grid = (unsigned)(a.n_tokens < most ? a.n_tokens : most);
   for_types(type, h_type, [&](auto e, auto h) {
     for_pieces<3>(n.ch, [&](auto ch) {
@@ -501,7 +521,8 @@ int launch_norm(const NormArgs &args, int32_t type, int32_t h_type, void *stream
   return (int)hipGetLastError();
 }
 
-// A workgroup per compute unit; as many teams in it as there are rows for, and the same number of rows for each.
+// A workgroup per compute unit; as many teams in it as there are rows for, and the same number of rows for each.  8192 rows of 1024:
+// 23.0 us with eight teams, 46.5 with one; 4096 of 4096 37.6 with two and 39.2.
 static NormShape norm_backward_shape(int width, bool branch) {
   return norm_shape(width, 3, [=](int ch) { return norm_backward_threads(ch, branch); });
 }

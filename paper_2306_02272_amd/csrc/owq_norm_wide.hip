@@ -1,7 +1,9 @@
 // Residual sum with norms, and the gradients, for rows that registers do not hold: a workgroup takes a row in rolled loops and
 // keeps what it comes back to in LDS, where a thread's pieces are its own.  (With the pieces of such a row in registers and every
 // loop over them unrolled the kernels are thousands of instructions that a row runs through once: fetching them bounds it.)
-// The formulas and the join of the waves' statistics are those of owq_norm.hip.
+// The formulas and the join of the waves' statistics are those of owq_norm.hip.  1000 rows of 16 384 fp16 take 30.5 us (25.7 by their
+// bytes at the rate of a large copy), 53 with both norms and a gate, their gradients 72 and 140 (32 and 39): the passes over a row stand
+// behind each other, and LDS holds one or two rows of a compute unit; the gradients read and write the sums over tokens for every row.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -133,14 +133,16 @@ struct ColumnSum<CH, true> {
   __device__ __forceinline__ void finish(float *mine, int k, int pitch, const RowPlace<CH> &at, int teams, float *store) {
     if (!mine || k < 0) return;            // the same for the whole workgroup
     float *to = mine + k * pitch;
+    if (teams == 1) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (at.count[c] > 0) put8(to, at.unit[c], v[c]);
+      return;
+    }
     const int columns = at.threads * 8 * CH;
     __syncthreads();
-    f32x4 *p = reinterpret_cast<f32x4 *>(store + at.team * columns);
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      p[2 * at.unit[c]] = (f32x4){v[c][0], v[c][1], v[c][2], v[c][3]};
-      p[2 * at.unit[c] + 1] = (f32x4){v[c][4], v[c][5], v[c][6], v[c][7]};
-    }
+    for (int c = 0; c < CH; ++c) put8(store + at.team * columns, at.unit[c], v[c]);
     __syncthreads();
     for (int i = 4 * (int)threadIdx.x; i < pitch; i += 4 * (int)blockDim.x) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};

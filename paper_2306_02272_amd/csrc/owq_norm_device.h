@@ -170,6 +170,13 @@ __device__ __forceinline__ void apply_norm(float (&x)[CH][8], const RowStat &s, 
   }
 }
 
+// Piece `unit` of a row of floats in LDS or in the workspace.
+__device__ __forceinline__ void put8(float *row, int unit, const float (&x)[8]) {
+  f32x4 *p = reinterpret_cast<f32x4 *>(row) + 2 * unit;
+  p[0] = (f32x4){x[0], x[1], x[2], x[3]};
+  p[1] = (f32x4){x[4], x[5], x[6], x[7]};
+}
+
 // size, and the gradient as size q + along n + all
 struct BackStat {
   float mean, size, along, all;

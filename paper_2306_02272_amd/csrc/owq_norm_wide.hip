@@ -12,11 +12,6 @@
 
 namespace owq {
 
-__device__ __forceinline__ void put8(float *row, int unit, const float (&x)[8]) {
-  f32x4 *p = reinterpret_cast<f32x4 *>(row) + 2 * unit;
-  p[0] = (f32x4){x[0], x[1], x[2], x[3]};
-  p[1] = (f32x4){x[4], x[5], x[6], x[7]};
-}
 __device__ __forceinline__ void get8(const float *row, int unit, float (&x)[8]) {
   const f32x4 *p = reinterpret_cast<const f32x4 *>(row) + 2 * unit;
   const f32x4 a = p[0], b = p[1];

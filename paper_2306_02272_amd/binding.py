@@ -509,8 +509,9 @@ def _ptr_of(x):
     return 0 if x is None else x.data_ptr()
 
 
-def _int32(x, n, what):
+def _int32(x, n, what, here=None):
     assert x.is_cuda and x.dtype is _TORCH.int32 and x.is_contiguous() and x.numel() >= n, (what, x.dtype, x.shape)
+    assert here is None or x.get_device() == here, (what, x.device)
     return x.data_ptr()
 
 
@@ -688,31 +689,41 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
 
 
 def _here(x):
-    """The work goes to the current device's current stream; refuses tensors of another device."""
-    assert x.is_cuda and x.get_device() == _TORCH._C._cuda_getDevice(), x.device
+    """The current device, to whose current stream the work goes; refuses x on another one.  The other tensors of a call are held
+    against it (the host is device -1)."""
+    here = _TORCH._C._cuda_getDevice() if x.is_cuda else None
+    assert x.get_device() == here, x.device
+    return here
 
 
-def _row_of(x, rows, width, dtype, what):
-    """Address and row stride of a CUDA tensor [rows, width] of `dtype`; (0, 0) for None."""
+def _row_of(x, rows, width, dtype, here, what):
+    """Address and row stride of a tensor [rows, width] of `dtype` on device `here`; (0, 0) for None."""
     if x is None:
         return 0, 0
     row, one = x.stride()
-    assert x.is_cuda and x.dtype is dtype and x.shape == (rows, width) and (one == 1 or width <= 1 or rows == 0), (what, x.dtype, x.shape)
+    assert x.get_device() == here and x.dtype is dtype and x.shape == (rows, width) and (one == 1 or width <= 1 or rows == 0), \
+        (what, x.device, x.dtype, x.shape)
     return x.data_ptr(), row
 
 
-def _packed(x, rows, width, dtype, what):
-    assert x.is_cuda and x.dtype is dtype and x.shape == (rows, width) and x.is_contiguous(), (what, x.dtype, x.shape)
+def _packed(x, rows, width, dtype, here, what):
+    assert x.get_device() == here and x.dtype is dtype and x.shape == (rows, width) and x.is_contiguous(), (what, x.device, x.dtype, x.shape)
     return x
 
 
-def _rng(rng, p):
+def _rng(rng, p, here):
     """Address of (seed, step); 0 where nothing is dropped."""
     if p == 0.0:
         return 0
     assert rng is not None, "dropout needs a tensor (seed, step)"
-    assert rng.is_cuda and rng.dtype is _TORCH.int64 and rng.is_contiguous() and rng.numel() == 2, (rng.dtype, rng.shape)
+    assert rng.get_device() == here and rng.dtype is _TORCH.int64 and rng.is_contiguous() and rng.numel() == 2, (rng.device, rng.dtype, rng.shape)
     return rng.data_ptr()
+
+
+def _workspace_bytes(x, here):
+    """Bytes of a given workspace."""
+    assert x.get_device() == here and x.is_contiguous(), (x.device, x.stride())
+    return x.numel() * x.element_size()
 
 
 def dropout(x, rng, p, site=0, residual=None, out=None):
@@ -721,11 +732,11 @@ def dropout(x, rng, p, site=0, residual=None, out=None):
     work runs; site: tells the droppings of a step apart.  The gradient of x: the same call on out's gradient, without residual."""
     torch = _torch()
     rows, width = x.shape
-    _here(x)
-    x_ptr, x_row = _row_of(x, rows, width, x.dtype, "x")
-    r_ptr, r_row = _row_of(residual, rows, width, x.dtype, "residual")
-    out = x.new_empty((rows, width)) if out is None else _packed(out, rows, width, x.dtype, "out")
-    status = lib().owq_dropout(x_ptr, r_ptr, _type_of(x, OWQ_TYPE_F32), rows, width, x_row, r_row, _rng(rng, p), p, site, out.data_ptr(),
+    here = _here(x)
+    x_ptr, x_row = _row_of(x, rows, width, x.dtype, here, "x")
+    r_ptr, r_row = _row_of(residual, rows, width, x.dtype, here, "residual")
+    out = x.new_empty((rows, width)) if out is None else _packed(out, rows, width, x.dtype, here, "out")
+    status = lib().owq_dropout(x_ptr, r_ptr, _type_of(x, OWQ_TYPE_F32), rows, width, x_row, r_row, _rng(rng, p, here), p, site, out.data_ptr(),
                                _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_dropout")
@@ -735,20 +746,20 @@ def dropout(x, rng, p, site=0, residual=None, out=None):
 _KINDS = {None: OWQ_NORM_NONE, "rms": OWQ_NORM_RMS, "layer": OWQ_NORM_LAYER}
 
 
-def _vector(x, width, dtype, what):
+def _vector(x, width, dtype, here, what):
     if x is None:
         return 0
-    assert x.is_cuda and x.dtype is dtype and x.is_contiguous() and x.numel() == width, (what, x.dtype, x.shape)
+    assert x.get_device() == here and x.dtype is dtype and x.is_contiguous() and x.numel() == width, (what, x.device, x.dtype, x.shape)
     return x.data_ptr()
 
 
-def _gate(gate, tokens, width, dtype):
+def _gate(gate, tokens, width, dtype, here):
     """(kind, address, row stride)"""
     if gate is None:
         return OWQ_GATE_NONE, 0, 0
     if gate.dim() == 1:
-        return OWQ_GATE_ROW, _vector(gate, width, dtype, "gate"), 0
-    return OWQ_GATE_TOKEN, *_row_of(gate, tokens, width, dtype, "gate")
+        return OWQ_GATE_ROW, _vector(gate, width, dtype, here, "gate"), 0
+    return OWQ_GATE_TOKEN, *_row_of(gate, tokens, width, dtype, here, "gate")
 
 
 def residual_norm(h, branch=None, gate=None, post=None, post_weight=None, post_bias=None, norm="rms", weight=None, bias=None, h_scale=1.0,
@@ -759,34 +770,34 @@ def residual_norm(h, branch=None, gate=None, post=None, post_weight=None, post_b
     `out`: packed tensors (total, y) to write to, total's may be h."""
     torch = _torch()
     tokens, width = h.shape
-    _here(h)
+    here = _here(h)
     h_dtype = h.dtype
     dtype = h_dtype
     if dtype is torch.float32:                     # the type of the rest
         rest = branch if branch is not None else weight if weight is not None else bias if bias is not None else None if out is None else out[1]
         dtype = dtype if rest is None else rest.dtype
-    h_ptr, h_row = _row_of(h, tokens, width, h_dtype, "h")
-    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, "branch")
-    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype)
+    h_ptr, h_row = _row_of(h, tokens, width, h_dtype, here, "h")
+    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, here, "branch")
+    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype, here)
     total, y = (None, None) if out is None else out
     if not want_total:
         total = None
     elif total is None:
         total = h.new_empty((tokens, width))
     else:
-        _packed(total, tokens, width, h_dtype, "out[0]")
+        _packed(total, tokens, width, h_dtype, here, "out[0]")
     if norm is None:
         y = None
     elif y is None:
         y = h.new_empty((tokens, width), dtype=dtype)
     else:
-        _packed(y, tokens, width, dtype, "out[1]")
+        _packed(y, tokens, width, dtype, here, "out[1]")
     desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _TYPES.get(h_dtype, 99), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale, branch_scale, p, h_row,
                       b_row, g_row, 0, 0, 0)
-    status = lib().owq_residual_norm(desc, h_ptr, b_ptr, g_ptr, 0 if post_weight is None else _vector(post_weight, width, dtype, "post_weight"),
-                                     0 if post_bias is None else _vector(post_bias, width, dtype, "post_bias"),
-                                     0 if weight is None else _vector(weight, width, dtype, "weight"),
-                                     0 if bias is None else _vector(bias, width, dtype, "bias"), _rng(rng, p),
+    status = lib().owq_residual_norm(desc, h_ptr, b_ptr, g_ptr, 0 if post_weight is None else _vector(post_weight, width, dtype, here, "post_weight"),
+                                     0 if post_bias is None else _vector(post_bias, width, dtype, here, "post_bias"),
+                                     0 if weight is None else _vector(weight, width, dtype, here, "weight"),
+                                     0 if bias is None else _vector(bias, width, dtype, here, "bias"), _rng(rng, p, here),
                                      0 if total is None else total.data_ptr(), 0 if y is None else y.data_ptr(), _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_residual_norm")
@@ -800,15 +811,15 @@ def residual_norm_backward(dy, dtotal, total, branch=None, gate=None, post=None,
     not there; those of weights, biases and a gate [width] are fp32."""
     torch = _torch()
     tokens, width = total.shape
-    _here(total)
+    here = _here(total)
     f32, h_dtype = torch.float32, total.dtype
     rest = dy if dy is not None else branch if branch is not None else weight
     dtype = h_dtype if rest is None else rest.dtype
-    t_ptr, t_row = _row_of(total, tokens, width, h_dtype, "total")
-    dt_ptr, dt_row = (0, 0) if dtotal is None else _row_of(dtotal, tokens, width, h_dtype, "dtotal")
-    dy_ptr, dy_row = (0, 0) if dy is None else _row_of(dy, tokens, width, dtype, "dy")
-    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, "branch")
-    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype)
+    t_ptr, t_row = _row_of(total, tokens, width, h_dtype, here, "total")
+    dt_ptr, dt_row = (0, 0) if dtotal is None else _row_of(dtotal, tokens, width, h_dtype, here, "dtotal")
+    dy_ptr, dy_row = (0, 0) if dy is None else _row_of(dy, tokens, width, dtype, here, "dy")
+    b_ptr, b_row = (0, 0) if branch is None else _row_of(branch, tokens, width, dtype, here, "branch")
+    kind, g_ptr, g_row = (OWQ_GATE_NONE, 0, 0) if gate is None else _gate(gate, tokens, width, dtype, here)
     new, shape = total.new_empty, (tokens, width)
     dh = new(shape)
     dbranch = None if branch is None else new(shape, dtype=dtype)
@@ -821,22 +832,22 @@ def residual_norm_backward(dy, dtotal, total, branch=None, gate=None, post=None,
     if kind == OWQ_GATE_TOKEN:
         dgate = new(shape, dtype=dtype)
     if bias is not None:
-        _vector(bias, width, dtype, "bias")
+        _vector(bias, width, dtype, here, "bias")
     desc = _NORM.pack(tokens, width, _TYPES.get(dtype, 99), _TYPES.get(h_dtype, 99), _KINDS[post], _KINDS[norm], kind, site, eps, h_scale,
                       branch_scale, p, 0, b_row, g_row, t_row, dy_row, dt_row)
     L = lib()
     n = 0
     if workspace is not None:
-        n = workspace.numel() * workspace.element_size()
+        n = _workspace_bytes(workspace, here)
     elif sums:
         need = C.c_size_t(0)
         _check(L.owq_residual_norm_backward_workspace_bytes(desc, need), "owq_residual_norm_backward_workspace_bytes")
         n = need.value
         workspace = new(n, dtype=torch.uint8)
     status = L.owq_residual_norm_backward(desc, dy_ptr, dt_ptr, t_ptr, b_ptr, g_ptr,
-                                          0 if post_weight is None else _vector(post_weight, width, dtype, "post_weight"),
-                                          0 if post_bias is None else _vector(post_bias, width, dtype, "post_bias"),
-                                          0 if weight is None else _vector(weight, width, dtype, "weight"), _rng(rng, p), dh.data_ptr(),
+                                          0 if post_weight is None else _vector(post_weight, width, dtype, here, "post_weight"),
+                                          0 if post_bias is None else _vector(post_bias, width, dtype, here, "post_bias"),
+                                          0 if weight is None else _vector(weight, width, dtype, here, "weight"), _rng(rng, p, here), dh.data_ptr(),
                                           _ptr_of(dbranch), _ptr_of(dgate), _ptr_of(dpw), _ptr_of(dpb), _ptr_of(dw), _ptr_of(db),
                                           _ptr_of(workspace), n, _current_stream(torch))
     if status != OWQ_OK:
@@ -850,14 +861,14 @@ def token_logprobs(logits, targets=None, scale=1.0, top=0):
     [3, rows]): stats are the largest logit, ln sum exp(scale (logit - largest)) and the entropy.  scale = 1 / temperature."""
     torch = _torch()
     rows, vocab = logits.shape
-    _here(logits)
-    ptr, row = _row_of(logits, rows, vocab, logits.dtype, "logits")
+    here = _here(logits)
+    ptr, row = _row_of(logits, rows, vocab, logits.dtype, here, "logits")
     f32 = torch.float32
     new = logits.new_empty
     logprob = None if targets is None else new(rows, dtype=f32)
     top_token, top_logprob = (new((rows, top), dtype=torch.int32), new((rows, top), dtype=f32)) if top else (None, None)
     stats = new((3, rows), dtype=f32)
-    t_ptr, lp_ptr = (0, 0) if targets is None else (_int32(targets, rows, "targets"), logprob.data_ptr())
+    t_ptr, lp_ptr = (0, 0) if targets is None else (_int32(targets, rows, "targets", here), logprob.data_ptr())
     tt_ptr, tl_ptr = (top_token.data_ptr(), top_logprob.data_ptr()) if top else (0, 0)
     status = lib().owq_token_logprobs(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row, t_ptr, scale, top, lp_ptr, tt_ptr, tl_ptr,
                                       stats.data_ptr(), _current_stream(torch))
@@ -871,13 +882,13 @@ def token_logprobs_backward(dlogprob, dentropy, logits, targets, stats, scale=1.
     logits; targets, stats, scale as in the forward.  Returns dlogits; `out`: where to write them, the logits themselves if packed."""
     torch = _torch()
     rows, vocab = logits.shape
-    _here(logits)
-    ptr, row = _row_of(logits, rows, vocab, logits.dtype, "logits")
+    here = _here(logits)
+    ptr, row = _row_of(logits, rows, vocab, logits.dtype, here, "logits")
     for x, n in ((dlogprob, rows), (dentropy, rows), (stats, 3 * rows)):
-        assert x is None or (x.is_cuda and x.dtype is torch.float32 and x.is_contiguous() and x.numel() == n)
-    out = logits.new_empty((rows, vocab)) if out is None else _packed(out, rows, vocab, logits.dtype, "out")
+        assert x is None or (x.get_device() == here and x.dtype is torch.float32 and x.is_contiguous() and x.numel() == n), (x.device, x.dtype, x.shape)
+    out = logits.new_empty((rows, vocab)) if out is None else _packed(out, rows, vocab, logits.dtype, here, "out")
     status = lib().owq_token_logprobs_backward(ptr, _type_of(logits, OWQ_TYPE_F32), rows, vocab, row,
-                                               0 if targets is None else _int32(targets, rows, "targets"), scale, stats.data_ptr(),
+                                               0 if targets is None else _int32(targets, rows, "targets", here), scale, stats.data_ptr(),
                                                _ptr_of(dlogprob), _ptr_of(dentropy), out.data_ptr(), _current_stream(torch))
     if status != OWQ_OK:
         raise OwqError(status, "owq_token_logprobs_backward")

@@ -515,6 +515,12 @@ def _int32(x, n, what, here=None):
     return x.data_ptr()
 
 
+def _workspace_bytes(x, here):
+    """Bytes of a workspace that the caller brings; it has to lie on device `here`."""
+    assert x.get_device() == here and x.is_contiguous(), (x.device, x.stride())
+    return x.numel() * x.element_size()
+
+
 def _rope_args(q, k, cos, sin, positions, wq, wk, eps, interleaved, dq=None, dk=None):
     """(description, tokens) after the checks that need the tensors; the library checks the rest."""
     torch = _torch()
@@ -565,12 +571,13 @@ def qk_norm_rope_backward(dq_out, dk_out, q, k, cos, sin, positions, wq=None, wk
     dwq = None if wq is None else q.new_empty(q.shape[2], dtype=f32)
     dwk = None if wk is None else q.new_empty(q.shape[2], dtype=f32)
     n = 0
-    if wq is not None or wk is not None:
-        if workspace is None:
-            need = C.c_size_t(0)
-            _check(lib().owq_qk_norm_rope_backward_workspace_bytes(desc, C.byref(need)), "owq_qk_norm_rope_backward_workspace_bytes")
-            workspace = q.new_empty(need.value, dtype=_TORCH.uint8)
-        n = workspace.numel()
+    if workspace is not None:
+        n = _workspace_bytes(workspace, q.get_device())
+    elif wq is not None or wk is not None:
+        need = C.c_size_t(0)
+        _check(lib().owq_qk_norm_rope_backward_workspace_bytes(desc, C.byref(need)), "owq_qk_norm_rope_backward_workspace_bytes")
+        n = need.value
+        workspace = q.new_empty(n, dtype=_TORCH.uint8)
     status = lib().owq_qk_norm_rope_backward(desc, dq_out.data_ptr(), dk_out.data_ptr(), q.data_ptr(), k.data_ptr(), _ptr_of(wq), _ptr_of(wk),
                                              cos.data_ptr(), sin.data_ptr(), _int32(positions, tokens, "positions"), dq.data_ptr(),
                                              dk.data_ptr(), _ptr_of(dwq), _ptr_of(dwk), _ptr_of(workspace), n, _current_stream(_TORCH))
@@ -656,7 +663,7 @@ def cache_attention(q, pages, page_table, starts, lengths, scale=None, window=0,
         n = need.value
         workspace = q.new_empty(n, dtype=torch.uint8) if n else None
     else:
-        n = workspace.numel()
+        n = _workspace_bytes(workspace, q.get_device())
     status = L.owq_cache_attention(desc, att, q.data_ptr(), pages.data_ptr(), _int32(page_table, n_seqs, "page_table"),
                                    _int32(starts, n_seqs + 1, "starts"), _int32(lengths, n_seqs, "lengths"), out.data_ptr(), _ptr_of(lse),
                                    _ptr_of(workspace), n, _current_stream(torch))
@@ -718,12 +725,6 @@ def _rng(rng, p, here):
     assert rng is not None, "dropout needs a tensor (seed, step)"
     assert rng.get_device() == here and rng.dtype is _TORCH.int64 and rng.is_contiguous() and rng.numel() == 2, (rng.device, rng.dtype, rng.shape)
     return rng.data_ptr()
-
-
-def _workspace_bytes(x, here):
-    """Bytes of a given workspace."""
-    assert x.get_device() == here and x.is_contiguous(), (x.device, x.stride())
-    return x.numel() * x.element_size()
 
 
 def dropout(x, rng, p, site=0, residual=None, out=None):
@@ -968,13 +969,15 @@ class OwqLinear:
         dww = torch.empty((self.d_out, k), dtype=torch.float32, device=dy.device) if want_dww else None
         if want_dww and k > 0:
             assert x is not None and x.dtype == torch.float16 and x.is_contiguous() and x.numel() == batch * self.d_in
+            assert x.get_device() == dy.get_device(), x.device
         if workspace is None:
-            workspace = torch.empty(owq_backward_workspace_bytes(self.handle, batch), dtype=torch.uint8, device=dy.device)
+            n = owq_backward_workspace_bytes(self.handle, batch)
+            workspace = torch.empty(n, dtype=torch.uint8, device=dy.device)
+        else:
+            n = _workspace_bytes(workspace, dy.get_device())
         owq_linear_backward(self.handle, dy.data_ptr(), x.data_ptr() if x is not None else 0,
                             dx.data_ptr() if want_dx else 0, dww.data_ptr() if (want_dww and k > 0) else 0, batch,
-                            workspace.data_ptr() if workspace is not None else 0,
-                            int(workspace.numel()) if workspace is not None else 0,
-                            _current_stream(torch))
+                            workspace.data_ptr(), n, _current_stream(torch))
         return dx, dww
 
     def close(self):

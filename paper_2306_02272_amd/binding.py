@@ -505,6 +505,11 @@ def _type_of(t, most=OWQ_TYPE_BF16):
     return n
 
 
+def _counts(rows, width):
+    """Refuses what the library's int32 counts do not hold: ctypes would cut it."""
+    assert (rows | width) < 0x80000000, (rows, width)
+
+
 def _ptr_of(x):
     return 0 if x is None else x.data_ptr()
 
@@ -677,6 +682,7 @@ def sample(logits, noise, temperature=None, top_k=None, top_p=None, min_p=None):
     temperature is 0); temperature, top_p, min_p fp32 and top_k int32 [rows] or None.  Returns (token int32, log-probability fp32)."""
     torch = _torch()
     rows, vocab = logits.shape
+    _counts(rows, vocab)
     row, one = logits.stride()
     f32 = torch.float32
     assert logits.is_cuda and (one == 1 or vocab == 1 or rows == 0), logits.stride()
@@ -734,6 +740,7 @@ def dropout(x, rng, p, site=0, residual=None, out=None):
     torch = _torch()
     rows, width = x.shape
     here = _here(x)
+    _counts(rows, width)
     x_ptr, x_row = _row_of(x, rows, width, x.dtype, here, "x")
     r_ptr, r_row = _row_of(residual, rows, width, x.dtype, here, "residual")
     out = x.new_empty((rows, width)) if out is None else _packed(out, rows, width, x.dtype, here, "out")
@@ -863,6 +870,7 @@ def token_logprobs(logits, targets=None, scale=1.0, top=0):
     torch = _torch()
     rows, vocab = logits.shape
     here = _here(logits)
+    _counts(rows, vocab)
     ptr, row = _row_of(logits, rows, vocab, logits.dtype, here, "logits")
     f32 = torch.float32
     new = logits.new_empty
@@ -884,6 +892,7 @@ def token_logprobs_backward(dlogprob, dentropy, logits, targets, stats, scale=1.
     torch = _torch()
     rows, vocab = logits.shape
     here = _here(logits)
+    _counts(rows, vocab)
     ptr, row = _row_of(logits, rows, vocab, logits.dtype, here, "logits")
     for x, n in ((dlogprob, rows), (dentropy, rows), (stats, 3 * rows)):
         assert x is None or (x.get_device() == here and x.dtype is torch.float32 and x.is_contiguous() and x.numel() == n), (x.device, x.dtype, x.shape)

@@ -25,17 +25,21 @@ namespace owq {
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kVanishes = -200.f;      // 2^-200 is 0 in binary32; keeps 0 times infinity out of the sums
 
-// Largest logit of a set, S and W about it.
+// Half of what two logits lie apart: no infinity however far that is, as the small scales that make numbers of it take any logits.
+// One rounding, of which no more is left than of the difference's.
+__device__ __forceinline__ float apart(float x, float from) { return __builtin_fmaf(0.5f, x, -0.5f * from); }
+
+// Largest logit of a set, S and W about it.  rate: 2 scale / ln 2, of what lies between logits by halves.
 struct Mass {
   float m, s, w;
   __device__ __forceinline__ void raise(float to, float rate) {
-    const float d = fmaxf((m - to) * rate, kVanishes), f = __builtin_amdgcn_exp2f(d);
+    const float d = fmaxf(apart(m, to) * rate, kVanishes), f = __builtin_amdgcn_exp2f(d);
     w = f * __builtin_fmaf(s, d, w);
     s *= f;
     m = to;
   }
   __device__ __forceinline__ void add(float v, float rate) {
-    const float d = (v - m) * rate, e = __builtin_amdgcn_exp2f(d);
+    const float d = apart(v, m) * rate, e = __builtin_amdgcn_exp2f(d);
     s += e;
     w = __builtin_fmaf(e, fmaxf(d, kVanishes), w);
   }
@@ -118,7 +122,7 @@ __device__ __forceinline__ bool store_row(const LogprobArgs &a, int64_t r, const
     a.stats[2 * (int64_t)a.n_rows + r] = good ? *log_s - kLn2 * (all.w / all.s) : nan;
     if (a.targets) {
       const int target = a.targets[r];
-      a.logprob[r] = (uint32_t)target < (uint32_t)a.vocab ? (logit_at<TYPE>(row, target) - all.m) * a.scale - *log_s : 0.f;
+      a.logprob[r] = (uint32_t)target < (uint32_t)a.vocab ? apart(logit_at<TYPE>(row, target), all.m) * (2.f * a.scale) - *log_s : 0.f;
     }
   }
   return good;
@@ -127,7 +131,7 @@ __device__ __forceinline__ bool store_row(const LogprobArgs &a, int64_t r, const
 template <int TYPE, int THREADS>
 __global__ __launch_bounds__(THREADS) void owq_logprob_kernel(LogprobArgs a) {
   __shared__ Mass part[THREADS / 64];
-  const float rate = kLog2e * a.scale;
+  const float rate = 2.f * kLog2e * a.scale;
   for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
     const void *row = logits_row<TYPE>(a, r);
     const RowView<TYPE> x(row, a.vocab);
@@ -243,7 +247,7 @@ __global__ __launch_bounds__(THREADS, 8) void owq_logprob_top_kernel(LogprobArgs
   __shared__ __attribute__((aligned(16))) u32 bins[kBins];
   __shared__ u32 winners[THREADS], n_winners, found[2];
   __shared__ Candidates<THREADS> list;
-  const float rate = kLog2e * a.scale;
+  const float rate = 2.f * kLog2e * a.scale;
   const int lane = threadIdx.x & 63;
   for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
     const void *row = logits_row<TYPE>(a, r);
@@ -264,7 +268,7 @@ __global__ __launch_bounds__(THREADS, 8) void owq_logprob_top_kernel(LogprobArgs
       __syncthreads();
       continue;
     }
-    const float d = (m - mine) * rate * 16.f;
+    const float d = apart(m, mine) * rate * 16.f;
     atomicAdd(&bins[d < (float)(kBins - 1) ? (u32)(int)d : kBins - 1], 1u);
     __syncthreads();
     u32 bin;
@@ -288,7 +292,7 @@ __global__ __launch_bounds__(THREADS, 8) void owq_logprob_top_kernel(LogprobArgs
       bin = (u32)who * 16u + (u32)__builtin_amdgcn_readlane((int)at, who);
     }
     // a little below the bin's edge, so that rounding leaves none of its logits out; the last bin is open
-    const float lo = bin >= kBins - 1 ? kLowest : fmaxf(m - ((float)(bin + 1) * 0.0625f / rate) * 1.00001f, kLowest);
+    const float lo = bin >= kBins - 1 ? kLowest : fmaxf(m - ((float)(bin + 1) * 0.125f / rate) * 1.00001f, kLowest);
     if (mine >= lo) winners[atomicAdd(&n_winners, 1u)] = threadIdx.x;
     __syncthreads();
     const u32 n_won = n_winners;
@@ -326,7 +330,7 @@ __global__ __launch_bounds__(THREADS, 8) void owq_logprob_top_kernel(LogprobArgs
         for (int i = 0; i < 4; ++i) rank += list.entry[j + i] > me ? 1u : 0u;      // past the end: 0, before nothing
       if (rank < (u32)a.top) {
         a.top_token[out + rank] = (int32_t)entry_at(me);
-        a.top_logprob[out + rank] = (entry_logit(me) - m) * a.scale - log_s;
+        a.top_logprob[out + rank] = apart(entry_logit(me), m) * (2.f * a.scale) - log_s;
       }
     }
     no_tokens<TYPE>(a, out, (int)n, -__builtin_inff());
@@ -369,7 +373,7 @@ int launch_logprobs(const LogprobArgs &a, int32_t type, void *stream) {
 // A workgroup takes pieces blockIdx.x 256 + thread, ... of rows blockIdx.y, ...
 template <class E>
 __global__ __launch_bounds__(256) void owq_logprob_backward_kernel(LogprobBackwardArgs a) {
-  const float rate = kLog2e * a.scale;
+  const float rate = 2.f * kLog2e * a.scale;
   const int units = (a.vocab + 7) >> 3;
   for (int64_t r = blockIdx.y; r < a.n_rows; r += gridDim.y) {
     const void *row = row_at<E>(a.logits, r, a.logits_row);
@@ -391,7 +395,7 @@ __global__ __launch_bounds__(256) void owq_logprob_backward_kernel(LogprobBackwa
         p.get(f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float l = __builtin_fmaf(f[j] - m, rate, -log2_s);
+          const float l = __builtin_fmaf(apart(f[j], m), rate, -log2_s);
           f[j] = __builtin_amdgcn_exp2f(l) * __builtin_fmaf(c1, fmaxf(l, kVanishes), c0);
         }
         if (counted && u == target >> 3) {

@@ -86,11 +86,11 @@ class Model:
         lp = B.token_logprobs(self.forward(tokens, rng)[0], targets)[0]
         return -lp.sum().item() / max(1, int((targets >= 0).sum()))
 
-    def gradients(self, tokens, targets, rng):
-        """(loss, gradients of the layers' weak columns in the order of layers(), of the vectors, of the embedded tokens)."""
+    def step(self, tokens, targets, count, rng):
+        """(log-probabilities, gradients of SCALE times the loss: of the layers' weak columns in the order of layers(), of the vectors, of
+        the embedded tokens), where `count` targets are counted.  Waits for nothing, so that a graph can hold it."""
         logits, (h, y, kept) = self.forward(tokens, rng)
         lp, _, _, stats = B.token_logprobs(logits, targets)
-        count = max(1, int((targets >= 0).sum()))
         dlp = torch.full_like(lp, -SCALE / count)
         dlogits = B.token_logprobs_backward(dlp, None, logits, targets, stats, out=logits)
         dy, dhead = self.head.linear.backward(dlogits, y)
@@ -105,6 +105,12 @@ class Model:
             vectors[i] = {"gate": dgate, "post": dpost, "norm": dnorm}
         dh, *_, dfirst, _ = B.residual_norm_backward(dy, dtotal, h, weight=self.first)
         vectors["first"] = dfirst
+        return lp, weak, vectors, dh
+
+    def gradients(self, tokens, targets, rng):
+        """(loss, its gradients in the order of step())."""
+        count = max(1, int((targets >= 0).sum()))
+        lp, weak, vectors, dh = self.step(tokens, targets, count, rng)
         unscaled = {i: v / SCALE if torch.is_tensor(v) else {k: g / SCALE for k, g in v.items()} for i, v in vectors.items()}
         return -lp.sum().item() / count, [g / SCALE for g in weak], unscaled, dh / SCALE
 

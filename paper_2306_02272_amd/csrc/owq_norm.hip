@@ -10,10 +10,10 @@
 //
 // What bounds it, with the rows' bytes at the rate of a large copy (5.1 TB/s) in brackets: one row of 4096 3.3 us (a load, a
 // reduction, a store behind each other); 4096 rows of 4096 fp16, layer norm, 24 to 28 us (26.3; reads and writes of memory); 1021
-// rows of 9216 with both norms and the gate, fp32 residual, 26 to 32 (22.2; 84 registers, nine waves per compute unit's
-// workgroup).  Gradients: 4096 rows of 4096 with dropout 34 + 4 us (32.9: memory, and 8 MB of partial sums written and read);
-// 777 rows of 5003 with both norms and the gate 30 + 4 (9.2: ten waves per compute unit, one row behind the other in each;
-// vector instructions take a quarter of the cycles).
+// rows of 9216 with both norms and the gate, fp32 residual, 26 to 32 (22.2; 165 registers: one workgroup of nine waves at work on a
+// compute unit, vector instructions in 36 % of the cycles).  Gradients: 4096 rows of 4096 with dropout 34 + 4 us (32.9: memory, and 8 MB of partial sums written and read);
+// 777 rows of 5003 with both norms and the gate 30 + 4 (9.2: 163 registers, ten waves per compute unit, one row behind the other in each;
+// vector instructions in 42 % of the cycles).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -102,9 +102,10 @@ __global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : (POST ? 6 : 8) - (Pi
 // to the row's mean: sum q (x - mean) = sum_w (Q_w + (c_w - mean) q_w), so that one barrier serves the statistics and both means.
 //
 // A workgroup of at most 1024 threads is as many teams as fit; team i of workgroup k takes rows (k teams + i) + steps of all
-// teams, and asks for its next row before it works on this one (CH = 1).  What it adds up over its rows stays in registers, as a
+// teams.  With one or two pieces a thread it asks for its next row before it works on this one, but where a norm of the branch meets a
+// gate only with one piece and a residual in 16 bits.  With one piece what it adds up over its rows stays in registers, as a
 // thread owns its columns; at the end the teams' are added through LDS and left as one row of the workspace, which a second
-// kernel adds up in order.  Two pieces a thread leave no registers for that: their sums are kept in LDS, and those that it does
+// kernel adds up in order.  Two and three pieces a thread leave no registers for that: their sums are kept in LDS, and those that it does
 // not hold in the workspace's row from the start.
 
 // Most threads of a workgroup: 128 registers for a thread, or 168 with the branch's side.  1021 rows of 8192 with both norms and the
@@ -112,7 +113,7 @@ __global__ __launch_bounds__(norm_threads(CH), CH > 1 ? 1 : (POST ? 6 : 8) - (Pi
 // 8192 without the branch's side 38.0 with one piece and 1024 threads, 43.1 with two and 512.
 constexpr int norm_backward_threads(int ch, bool branch) { return ch > 1 ? 512 : branch ? 640 : 1024; }
 
-constexpr int kSumsLds = 38912;      // floats for the sums of two pieces a thread
+constexpr int kSumsLds = 38912;      // floats for the sums of two and three pieces a thread
 
 template <int CH, bool REGISTERS>
 struct ColumnSum;

@@ -1,9 +1,11 @@
 // Residual sum with norms, and the gradients, for rows that registers do not hold: a workgroup takes a row in rolled loops and
 // keeps what it comes back to in LDS, where a thread's pieces are its own.  (With the pieces of such a row in registers and every
 // loop over them unrolled the kernels are thousands of instructions that a row runs through once: fetching them bounds it.)
-// The formulas and the join of the waves' statistics are those of owq_norm.hip.  1000 rows of 16 384 fp16 take 30.5 us (25.7 by their
-// bytes at the rate of a large copy), 53 with both norms and a gate, their gradients 72 and 140 (32 and 39): the passes over a row stand
-// behind each other, and LDS holds one or two rows of a compute unit; the gradients read and write the sums over tokens for every row.
+// The formulas and the join of the waves' statistics are those of owq_norm.hip.  1000 rows of 16 384 fp16 take 26 to 30 us (25.7 by their
+// bytes at the rate of a large copy), 46 to 53 with both norms and a gate, their gradients 70 and 140 (32 and 39): the passes over a row stand
+// behind each other, and a compute unit has one or two rows at work: LDS holds two of the forward's and one of the gradients', and the
+// 132 to 134 registers of a forward with a norm of the branch let one workgroup of eight waves in; the gradients read and write the sums
+// over tokens for every row.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -391,7 +393,7 @@ static void for_types(int type, int h_type, F &&f) {
 }
 
 int launch_norm_wide(const NormArgs &a, int32_t type, int32_t h_type, void *stream) {
-  const unsigned grid = (unsigned)(a.n_tokens < 512 ? a.n_tokens : 512);      // two fit a compute unit's LDS
+  const unsigned grid = (unsigned)(a.n_tokens < 512 ? a.n_tokens : 512);      // two a compute unit; with a norm of the branch the second waits for the first (registers)
   const hipStream_t s = static_cast<hipStream_t>(stream);
   for_types(type, h_type, [&](auto e, auto h) {
     if (a.post != OWQ_NORM_NONE) owq_norm_wide_kernel<decltype(e), decltype(h), true><<<grid, 512, 0, s>>>(a);

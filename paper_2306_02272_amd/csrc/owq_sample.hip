@@ -342,7 +342,8 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     __syncthreads();
     // a little below the bin's edge, so that rounding leaves none of its logits out; the last bin is open
     const u32 bin = sh.digit;
-    lo = bin >= kBins - 1 || all < (u32)k ? -3.402823466e38f : top - ((float)(bin + 1) * 0.0625f / rate) * 1.00001f;
+    constexpr float kLowest = -3.402823466e38f;      // not -infinity: what stands past the row's end is no candidate
+    lo = bin >= kBins - 1 || all < (u32)k ? kLowest : fmaxf(top - ((float)(bin + 1) * 0.0625f / rate) * 1.00001f, kLowest);
   } else if (by_p || long_k) {
     clear_bins(sh);
   }

@@ -17,6 +17,10 @@ __device__ __forceinline__ float logit_of(u32 key) {
   return __builtin_bit_cast(float, (key & 0x80000000u) ? key & 0x7fffffffu : ~key);
 }
 
+// Half of what x lies above `from`: no infinity however far that is, as the small scales and large temperatures that make numbers of
+// it take any logits.  One rounding, of which no more is left than of the difference's.
+__device__ __forceinline__ float apart(float x, float from) { return __builtin_fmaf(0.5f, x, -0.5f * from); }
+
 template <int TYPE>
 __device__ __forceinline__ float logit_at(const void *row, int i) {
   if (TYPE == OWQ_TYPE_F32) return static_cast<const float *>(row)[i];

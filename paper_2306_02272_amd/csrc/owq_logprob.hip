@@ -30,10 +30,6 @@ namespace owq {
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kVanishes = -200.f;      // 2^-200 is 0 in binary32; keeps 0 times infinity out of the sums
 
-// Half of what two logits lie apart: no infinity however far that is, as the small scales that make numbers of it take any logits.
-// One rounding, of which no more is left than of the difference's.
-__device__ __forceinline__ float apart(float x, float from) { return __builtin_fmaf(0.5f, x, -0.5f * from); }
-
 // Largest logit of a set, S and W about it.  rate: 2 scale / ln 2, of what lies between logits by halves.
 struct Mass {
   float m, s, w;

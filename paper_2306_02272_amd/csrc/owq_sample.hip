@@ -71,7 +71,7 @@ __device__ __forceinline__ float log2_of(float x) {
 }
 
 __device__ __forceinline__ u32 mass_of(float x, float top, float rate) {
-  return (u32)(__builtin_amdgcn_exp2f((x - top) * rate) * kMassUnit);
+  return (u32)(__builtin_amdgcn_exp2f(apart(x, top) * rate) * kMassUnit);
 }
 
 // Descends the keys by eight bits at a time.  By count: the key of the `want`-th largest.  By mass: the largest key
@@ -313,14 +313,15 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   float mine = bottom;
   x.each([&](float v) { mine = fmaxf(mine, v); });
   const float t = a.temperature ? a.temperature[r] : 1.f;
-  const float rate = kLog2e / (t > 0.f ? t : 1.f);
+  const float rate = 2.f * kLog2e / (t > 0.f ? t : 1.f);      // of what lies between logits by halves
   const int k = a.top_k ? a.top_k[r] : 0;
   const float p = a.top_p ? a.top_p[r] : 1.f, mp = a.min_p ? a.min_p[r] : 0.f;
   const float top = block_top(mine, sh);
   const bool by_k = t > 0.f && k >= 1 && k < a.vocab, short_k = by_k && k <= kList / 2, long_k = by_k && !short_k, by_p = t > 0.f && !by_k && p < 1.f;
   // Everything is measured from the largest logit, in log2 of the probability: sums with a logit itself would round at its size,
   // not at the difference's, and overflow at small temperatures.
-  auto below = [&](float v) { return (top - v) * rate; };
+  const float half_top = 0.5f * top;
+  auto below = [&](float v) { return __builtin_fmaf(-0.5f, v, half_top) * rate; };      // apart(top, v)
   const float reach = mp > 0.f ? -log2_of(mp) : __builtin_inff();       // z >= max z + ln min_p
   auto likely = [&](float v) { return below(v) <= reach || v == top; };
   clear_lists(sh);
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
     // a little below the bin's edge, so that rounding leaves none of its logits out; the last bin is open
     const u32 bin = sh.digit;
     constexpr float kLowest = -3.402823466e38f;      // not -infinity: what stands past the row's end is no candidate
-    lo = bin >= kBins - 1 || all < (u32)k ? kLowest : fmaxf(top - ((float)(bin + 1) * 0.0625f / rate) * 1.00001f, kLowest);
+    lo = bin >= kBins - 1 || all < (u32)k ? kLowest : fmaxf(top - ((float)(bin + 1) * 0.125f / rate) * 1.00001f, kLowest);
   } else if (by_p || long_k) {
     clear_bins(sh);
   }
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
 
   const float *noise = a.noise + (int64_t)r * a.noise_row;
   auto score = [&](u64 e) {
-    return entry_of(__builtin_fmaf(entry_logit(e) - top, rate, -log2_of(noise[entry_at(e)])), entry_at(e));
+    return entry_of(__builtin_fmaf(apart(entry_logit(e), top), rate, -log2_of(noise[entry_at(e)])), entry_at(e));
   };
   u64 best = 0;
   Cut cut = {key_of(bottom) + 1u, 0xffffffffu};
@@ -544,7 +545,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
       for (int i = 0; i < 16; ++i) u[i] = noise[min(index(i), a.vocab - 1)];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const u64 o = entry_of(__builtin_fmaf(v[i] - top, rate, -log2_of(u[i])), (u32)index(i));
+        const u64 o = entry_of(__builtin_fmaf(apart(v[i], top), rate, -log2_of(u[i])), (u32)index(i));
         best = ((bits >> i) & 1u) && o > best ? o : best;
       }
     });
@@ -553,7 +554,7 @@ __global__ __launch_bounds__(kSampleThreads) void owq_sample_kernel(SampleArgs a
   if (threadIdx.x == 0) {
     const int token = (int)(0xffffffffu - (u32)best);
     a.token[r] = token;
-    if (a.logprob) a.logprob[r] = (logit_at<TYPE>(row, token) - top) * (rate * kLn2) - __builtin_logf(total);
+    if (a.logprob) a.logprob[r] = apart(logit_at<TYPE>(row, token), top) * (rate * kLn2) - __builtin_logf(total);
   }
 }
 
